@@ -61,6 +61,8 @@ extern "C" {
 #define ITQ3S_FLAG_BAD_CODE 8u  /* decode: a code outside {0,1,2} was met (dequantize checks both
                                    planes; matmul checks the high plane only and treats a low-plane
                                    3 as digit +2; itq3s_matmul_sub up to 64 rows: as +3)           */
+#define ITQ3S_FLAG_BAD_SLOT 32u /* cache: a slot or page beyond the cache's last, or a length beyond the page table: nothing
+                                   is read or written there (see the calls)                        */
 #define ITQ3S_FLAG_ACT_RANGE 16u /* matmul: a rotated activation left the fp16 range (see itq3s_matmul);
                                    the outputs that depend on that 256-channel chunk are Inf or NaN */
 
@@ -226,6 +228,104 @@ int itq3s_dequantize_sub(const uint32_t *codes, const uint32_t *scales, const ui
 int itq3s_matmul_sub(const uint32_t *codes, const uint32_t *scales, const uint32_t *subscales, int64_t N, int64_t K,
                      const void *X, int64_t M, int64_t ldx, void *Y, int y_dtype, int64_t ldy, void *workspace,
                      size_t workspace_bytes, uint32_t *status_flags, void *stream);
+
+/* ---- The attention half of a layer: what runs between the q/k/v product and the output product.
+ *
+ * Rows of heads: Q is T x (q_heads * head_dim), K and V are T x (kv_heads * head_dim), row-major, one token a row, its heads
+ * beside each other -- what itq3s_matmul_grouped leaves in Y.  Row strides in elements; pointers 16-byte aligned, strides a
+ * multiple of 16 bytes (also columns of a wider buffer).  head_dim 64, 128 or 256 (ITQ3S_ERR_SHAPE else); q_heads a multiple of
+ * kv_heads: query head h reads kv head h / (q_heads / kv_heads).  kv_heads up to 1024, q_heads up to 65536.
+ *
+ * The cache.  A row of it is one token of one kv head, for keys and for values: head_dim values x are turned, w = H x with the
+ * orthonormal Walsh-Hadamard matrix of head_dim points in natural order (an outlier channel is spread over the row, so one
+ * step serves it whole), and coded in 4 bits: step s = max|w| / 7.5 rounded to fp16 (through fp32), digits
+ * c = floor(w / s + 1/2) within -8..7.  The row stands for x~ = H (s c).  w, max and digits are computed in 64 bits: digits depend on
+ * the input alone.  0.516 bytes a value at head_dim 128.  A row with a NaN or infinity is stored as zeros
+ * (ITQ3S_FLAG_NONFINITE), a step beyond fp16 as 65504 (ITQ3S_FLAG_SCALE_SAT); rows whose largest |w| is below 2.2e-7 are zeros,
+ * and steps below 6e-5 have fewer bits.
+ *   Blocks of 32 tokens of one kv head, 32 * head_dim + 128 bytes (D = head_dim; t = 0..31 the token of the block):
+ *     keys   at 0     : digit of channel 8 w + j of token t in word t * D / 8 + w, nibble (j >> 1) + 4 (j & 1)
+ *     values at 16 D  : token t = 16 a + 4 g + b, channel 64 h + 32 p + 16 n + c: nibble n of byte
+ *                       1024 h + 16 (16 g + c) + 8 p + 4 a + 2 (b & 1) + (b >> 1)
+ *     steps  at 32 D  : word t = fp16 bits of the key's step | fp16 bits of the value's step << 16
+ *     nibbles hold c + 8; words are little-endian
+ *   Pages of page_tokens tokens (a power of two, 32 .. 65536): page p holds, head after head, its page_tokens / 32 blocks one after
+ *   the other.  Slot i is token i % page_tokens of page i / page_tokens.
+ * The struct is a HOST descriptor (read during the call, not kept); data is device memory of itq3s_cache_bytes(), 128-byte aligned.
+ * The library keeps no other state: lengths, page tables and slots are the caller's, in device memory, and are read
+ * when the kernels run, so that a captured call follows them from replay to replay. */
+typedef struct itq3s_cache {
+    void *data;
+    int64_t pages; /* at most 2^31 - 1 */
+    int page_tokens;
+    int kv_heads;
+    int head_dim;
+} itq3s_cache;
+/* pages * kv_heads * (page_tokens / 32) * (32 * head_dim + 128); 0 if a size is not allowed, or beyond 2^48. */
+size_t itq3s_cache_bytes(int64_t pages, int page_tokens, int kv_heads, int head_dim);
+
+/* Frequencies of the position rotation, on the HOST: freq[i] = base^(-2 i / rot), i < rot / 2, in 64 bits.  For contexts longer than
+ * the trained one, factor > 1 slows them down: all of them by factor (trained_tokens = 0), or by parts:
+ * a frequency that makes n = trained_tokens * freq / (2 pi) turns over the trained length stays as it is for n >= fast_turns, is
+ * divided by factor for n <= slow_turns, and between them goes over in proportion to n.
+ *   rot even, 2..256;  base > 0, factor > 0, and for trained_tokens > 0: 0 <= slow_turns < fast_turns (ITQ3S_ERR_SHAPE else) */
+int itq3s_rope_frequencies(int rot, double base, double factor, int64_t trained_tokens, double slow_turns, double fast_turns, double *freq);
+
+/* Norm and position rotation of the query and key heads, keys and values into the cache, in one launch.
+ * Every head x of Q and K, in this order:
+ *   norm (q_norm, k_norm not NULL)  x * w / sqrt(mean(x^2) + eps), w the head_dim weights, fp32, shared by the heads
+ *   rotation (rot > 0)  pairs (x_a, x_b) of the first rot channels -- (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved --
+ *                       become gain * (x_a cos - x_b sin, x_b cos + x_a sin), angle positions[t] * freq[i] in 64 bits
+ * then Q_out and K_out receive the results (rounded once; each may be its input with the same stride), and the cache the
+ * codes of the rotated keys (unrounded) and of V at slots[t].
+ *   Q      may be NULL: no queries (Q_out, q_heads unused)
+ *   K      may be NULL where there is no cache;  K_out may be NULL where there is one
+ *   V      required with a cache, NULL without
+ *   cache  may be NULL: norm and rotation only (slots unused)
+ *   slots  device, T int64: where token t goes.  Negative: nowhere (padding; its Q_out and K_out are written all the same).  Beyond
+ *          the cache: nowhere, ITQ3S_FLAG_BAD_SLOT.  Two tokens of one call at one slot leave there digits of either.
+ *   positions device, T int32 (not needed if rot is 0);  freq device, rot / 2 doubles
+ *   rot a multiple of 16, at most head_dim;  in_dtype of Q, K and V, out_dtype of Q_out and K_out;  T up to 2^31 - 1 */
+int itq3s_cache_append(const void *Q, int64_t ldq, int q_heads, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int in_dtype,
+                       int kv_heads, int head_dim, const float *q_norm, const float *k_norm, float eps, const int32_t *positions,
+                       const double *freq, int rot, int interleaved, float gain, void *Q_out, int64_t ldqo, void *K_out, int64_t ldko,
+                       int out_dtype, const itq3s_cache *cache, const int64_t *slots, uint32_t *status_flags, void *stream);
+
+/* Rows of the cache as the values that they stand for: K_out[t], V_out[t] (T x (kv_heads * head_dim) of out_dtype) of slots[t], in
+ * any order, any number of times.  A negative slot gives zeros, one beyond the cache zeros and ITQ3S_FLAG_BAD_SLOT. */
+int itq3s_cache_read(const itq3s_cache *cache, const int64_t *slots, int64_t T, void *K_out, int64_t ldk, void *V_out, int64_t ldv,
+                     int out_dtype, uint32_t *status_flags, void *stream);
+
+/* Attention of the last rows of every sequence over the cache, which holds those rows' own keys already: decode (one row a
+ * sequence), several rows at once, chunks of a prompt.  Sequence s has rows q_starts[s] .. q_starts[s + 1] - 1 of Q and out, n of them, and
+ * kv_lens[s] tokens in the cache, token j in page pages[s * ld_pages + j / page_tokens]; its row i sees the tokens
+ * j <= kv_lens[s] - n + i:
+ *   out = sum_j p_j v~_j,  p = softmax_j(scale q . k~_j)     (fp16; weights and digits multiply in fp16, sums are fp32)
+ * A row that sees no token is zeros.  Rows of no sequence stay as they were.  A query with a NaN or infinity gives NaN.
+ *   Q, out   device, T x (q_heads * head_dim) fp16
+ *   q_starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it);  kv_lens device, seqs int32 (negative: 0; more
+ *            than ld_pages * page_tokens: that much, ITQ3S_FLAG_BAD_SLOT);  pages device, int32: a page that is not of
+ *            the cache is taken for tokens that nobody sees, ITQ3S_FLAG_BAD_SLOT; entries behind a sequence's last token are not read
+ *   max_q, max_kv  the most rows and tokens of a sequence that the work is cut up for.  Longer sequences are computed all the same,
+ *            slower; with max_q above T, T is meant
+ *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  scale finite
+ *   workspace device, 256-byte aligned, itq3s_cache_attention_workspace_bytes() of the same sizes (never 0); as for itq3s_matmul */
+size_t itq3s_cache_attention_workspace_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv);
+int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, const itq3s_cache *cache, const int32_t *q_starts,
+                          const int32_t *kv_lens, int64_t seqs, const int32_t *pages, int64_t ld_pages, int64_t max_q, int64_t max_kv,
+                          float scale, void *out, int64_t ldo, void *workspace, size_t workspace_bytes, uint32_t *status_flags, void *stream);
+
+/* Attention of whole prompts over their own keys and values, as they come out of the product and the rotation, fp16: sequence s
+ * has rows starts[s] .. starts[s + 1] - 1 of Q, K, V and out; its row i sees its rows j <= i, or all of them if causal is 0.
+ * Weights multiply in fp16, sums are fp32.  Rows of no sequence are neither read nor written.  In a sequence, a NaN or infinity
+ * in K or V makes NaN of the rows that see it, and may of rows before it as well.
+ *   Q, out T x (q_heads * head_dim), K, V T x (kv_heads * head_dim), all fp16;  out must not overlap the inputs
+ *   starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it)
+ *   max_len  the most rows of a sequence that the work is cut up for (longer ones are computed all the same, slower)
+ *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  scale finite;  no workspace */
+int itq3s_prompt_attention(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int q_heads,
+                           int kv_heads, int head_dim, const int32_t *starts, int64_t seqs, int64_t max_len, int causal, float scale,
+                           void *out, int64_t ldo, void *stream);
 
 /* Static text for a status code.  Never NULL. */
 const char *itq3s_strerror(int status);

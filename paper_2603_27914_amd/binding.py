@@ -4,6 +4,7 @@ Argument marshalling only: torch tensors supply device memory and the current HI
 step of the computation runs in the library's kernels.  There is no CPU fallback -- if the shared
 library is missing or a call fails, an exception is raised.
 """
+import collections
 import ctypes
 import os
 
@@ -13,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libitq3s.so")
 
 F32, F16 = 0, 1
-FLAG_NONFINITE, FLAG_SCALE_SAT, FLAG_Z_CLAMP, FLAG_BAD_CODE, FLAG_ACT_RANGE = 1, 2, 4, 8, 16
+FLAG_NONFINITE, FLAG_SCALE_SAT, FLAG_Z_CLAMP, FLAG_BAD_CODE, FLAG_ACT_RANGE, FLAG_BAD_SLOT = 1, 2, 4, 8, 16, 32
 
 EXPORTS = [
     "itq3s_codes_bytes",
@@ -29,6 +30,13 @@ EXPORTS = [
     "itq3s_quantize_sub",
     "itq3s_dequantize_sub",
     "itq3s_matmul_sub",
+    "itq3s_cache_bytes",
+    "itq3s_rope_frequencies",
+    "itq3s_cache_append",
+    "itq3s_cache_read",
+    "itq3s_cache_attention_workspace_bytes",
+    "itq3s_cache_attention",
+    "itq3s_prompt_attention",
     "itq3s_matmul_grouped_timed",
     "itq3s_matmul_timed",
     "itq3s_matmul_weight_side",
@@ -98,6 +106,21 @@ def lib():
         L.itq3s_matmul_weight_side_timed.argtypes = L.itq3s_matmul_weight_side.argtypes + [ctypes.POINTER(ctypes.c_float)]
         L.itq3s_read_probe.restype = ci
         L.itq3s_read_probe.argtypes = [vp, sz, vp, vp]
+        fl, dp, cache = ctypes.c_float, ctypes.c_double, ctypes.POINTER(CacheDesc)
+        L.itq3s_cache_bytes.restype = sz
+        L.itq3s_cache_bytes.argtypes = [i64, ci, ci, ci]
+        L.itq3s_rope_frequencies.restype = ci
+        L.itq3s_rope_frequencies.argtypes = [ci, dp, dp, i64, dp, dp, vp]
+        L.itq3s_cache_append.restype = ci
+        L.itq3s_cache_append.argtypes = [vp, i64, ci, vp, i64, vp, i64, i64, ci, ci, ci, vp, vp, fl, vp, vp, ci, ci, fl, vp, i64, vp, i64, ci, cache, vp, vp, vp]
+        L.itq3s_cache_read.restype = ci
+        L.itq3s_cache_read.argtypes = [cache, vp, i64, vp, i64, vp, i64, ci, vp, vp]
+        L.itq3s_cache_attention_workspace_bytes.restype = sz
+        L.itq3s_cache_attention_workspace_bytes.argtypes = [i64, i64, ci, ci, ci, i64, i64]
+        L.itq3s_cache_attention.restype = ci
+        L.itq3s_cache_attention.argtypes = [vp, i64, i64, ci, cache, vp, vp, i64, vp, i64, i64, i64, fl, vp, i64, vp, sz, vp, vp]
+        L.itq3s_prompt_attention.restype = ci
+        L.itq3s_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, i64, ci, ci, ci, vp, i64, i64, ci, fl, vp, i64, vp]
         L.itq3s_strerror.restype = ctypes.c_char_p
         L.itq3s_strerror.argtypes = [ci]
         L.itq3s_version.restype = ci
@@ -447,4 +470,256 @@ def itq3s_matmul_sub(codes, scales, subscales, N, K, X, dtype=torch.float32, out
         dtype = out.dtype
     _check(lib().itq3s_matmul_sub(_ptr(codes), _ptr(scales), _ptr(subscales), N, K, _ptr(X), M, X.stride(0), _ptr(out), F16 if dtype == torch.float16 else F32,
                                   out.stride(0), _ptr(workspace), workspace.numel() if workspace is not None else 0, _ptr(status_flags), _stream()))
+    return out
+
+
+# ---- the attention half of a layer: norm and rotation, the 4-bit cache, attention
+
+
+class CacheDesc(ctypes.Structure):
+    """struct itq3s_cache"""
+
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class Cache(collections.namedtuple("Cache", "data page_tokens kv_heads head_dim")):
+    """A cache of keys and values: a contiguous uint8 device tensor of whole pages, and its layout."""
+
+    __slots__ = ()
+
+    @property
+    def pages(self):
+        one = itq3s_cache_bytes(1, self.page_tokens, self.kv_heads, self.head_dim)
+        return self.data.numel() // one if one else 0
+
+
+def itq3s_cache_bytes(pages, page_tokens, kv_heads, head_dim):
+    return lib().itq3s_cache_bytes(pages, page_tokens, kv_heads, head_dim)
+
+
+def alloc_cache(pages, page_tokens, kv_heads, head_dim, device="cuda"):
+    """A cache of `pages` pages whose rows are all zeros."""
+    nbytes = itq3s_cache_bytes(pages, page_tokens, kv_heads, head_dim)
+    if nbytes == 0:
+        raise Itq3sError("bad shape: page_tokens a power of two from 32 to 65536, head_dim 64, 128 or 256, pages and kv_heads positive")
+    return Cache(torch.zeros(nbytes, dtype=torch.uint8, device=device), page_tokens, kv_heads, head_dim)
+
+
+def _need_cache(cache):
+    """-> the descriptor of a cache, checked against its tensor."""
+    data, page_tokens, kv_heads, head_dim = cache
+    if data.dtype != torch.uint8 or not data.is_contiguous():
+        raise Itq3sError("the cache's data must be a contiguous uint8 tensor")
+    one = itq3s_cache_bytes(1, page_tokens, kv_heads, head_dim)
+    if one == 0:
+        raise Itq3sError("bad cache: page_tokens a power of two from 32 to 65536, head_dim 64, 128 or 256, kv_heads positive")
+    pages, rest = divmod(data.numel(), one)
+    if pages == 0 or rest:
+        raise Itq3sError("the cache holds %d bytes: not whole pages of %d" % (data.numel(), one))
+    return CacheDesc(data.data_ptr(), pages, page_tokens, kv_heads, head_dim)
+
+
+def _need_here(*tensors):
+    """Device tensors, all on the current device, whose stream the call goes to."""
+    index = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise Itq3sError("libitq3s works on device memory only; got a CPU tensor")
+        if index is None:
+            index = _device()
+        if t.get_device() != index:
+            raise Itq3sError("every tensor of a call must be on the current device")
+
+
+def _need_rows(name, t, T, width, dtypes):
+    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] != T or t.shape[1] != width or t.dtype not in dtypes:
+        raise Itq3sError("%s must be %s [%d, %d] with unit column stride" % (name, "/".join(str(d)[6:] for d in dtypes), T, width))
+
+
+def _need_list(name, t, n, dtype):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise Itq3sError("%s must be a contiguous %s tensor of %d" % (name, str(dtype)[6:], n))
+
+
+_FLOATS, _HALF = (torch.float32, torch.float16), (torch.float16,)
+
+
+def _ld(t):
+    """Row stride; a single row's has no meaning to torch."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def itq3s_rope_frequencies(rot, base=10000.0, factor=1.0, trained_tokens=0, slow_turns=1.0, fast_turns=4.0):
+    """Frequencies of the position rotation of `rot` channels as a float64 CPU tensor [rot / 2] (move it to the device once):
+    base^(-2i/rot), divided by `factor` for longer contexts, all of them or, with trained_tokens, by parts."""
+    if not 0 < rot <= 256 or rot % 2:
+        raise Itq3sError("rot must be even and at most 256")
+    freq = torch.empty(rot // 2, dtype=torch.float64)
+    _check(lib().itq3s_rope_frequencies(rot, base, factor, trained_tokens, slow_turns, fast_turns, freq.data_ptr()))
+    return freq
+
+
+def itq3s_cache_append(q, k, v, positions=None, freq=None, cache=None, slots=None, head_dim=None, interleaved=False, gain=1.0, q_norm=None, k_norm=None, eps=1e-6,
+                       q_out=None, k_out=None, dtype=torch.float16, status_flags=None):
+    """Norm and position rotation of the heads of q [T, q_heads * head_dim] and k [T, kv_heads * head_dim] (float32 or
+    float16), k and v into the cache at slots [T] (int64; negative: nowhere).  -> (q_out, k_out).
+
+    freq: float64 [rot / 2] (the first `rot` channels of a head are rotated) or None; positions: int32 [T].
+    q_norm, k_norm: float32 [head_dim] or None.  q may be None; k and v may be without a cache (head_dim is needed then).
+    q_out: written if given, else allocated as `dtype`; k_out: likewise without a cache, with one only written if given."""
+    _need_here(q, k, v, positions, freq, cache.data if cache is not None else None, slots, q_norm, k_norm, q_out, k_out, status_flags)
+    first = q if q is not None else k
+    if first is None:
+        raise Itq3sError("q or k is needed")
+    if first.dim() != 2 or first.dtype not in _FLOATS:
+        raise Itq3sError("q and k must be float32/float16 [T, heads * head_dim] with unit column stride")
+    T, in_dtype = first.shape[0], (first.dtype,)
+    desc, kv_heads = None, 1
+    if cache is not None:
+        desc = _need_cache(cache)
+        if k is None or v is None or slots is None:
+            raise Itq3sError("a cache needs k, v and slots")
+        head_dim, kv_heads = cache.head_dim, cache.kv_heads
+        _need_list("slots", slots, T, torch.int64)
+        _need_rows("v", v, T, kv_heads * head_dim, in_dtype)
+    elif v is not None:
+        raise Itq3sError("v is only needed with a cache")
+    if head_dim not in (64, 128, 256):
+        raise Itq3sError("head_dim must be 64, 128 or 256")
+    q_heads = rot = 0
+    if k is not None:
+        if cache is None:
+            kv_heads = max(k.shape[-1] // head_dim, 1)
+        _need_rows("k", k, T, kv_heads * head_dim, in_dtype)
+        if k_out is None and cache is None:
+            k_out = torch.empty((T, kv_heads * head_dim), dtype=q_out.dtype if q_out is not None else dtype, device=k.device)
+    elif k_out is not None:
+        raise Itq3sError("k_out without k")
+    if q is not None:
+        q_heads = max(q.shape[-1] // head_dim, 1)
+        _need_rows("q", q, T, q_heads * head_dim, in_dtype)
+        if q_out is None:
+            q_out = torch.empty((T, q_heads * head_dim), dtype=k_out.dtype if k_out is not None else dtype, device=q.device)
+        _need_rows("q_out", q_out, T, q_heads * head_dim, _FLOATS)
+    elif q_out is not None:
+        raise Itq3sError("q_out without q")
+    if k_out is not None:
+        _need_rows("k_out", k_out, T, kv_heads * head_dim, _FLOATS if q_out is None else (q_out.dtype,))
+    if freq is not None:
+        if positions is None:
+            raise Itq3sError("a rotation needs positions")
+        _need_list("freq", freq, freq.numel(), torch.float64)
+        _need_list("positions", positions, T, torch.int32)
+        rot = 2 * freq.numel()
+    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None:
+            _need_list(name, w, head_dim, torch.float32)
+    _need_flags(status_flags)
+    out = q_out if q_out is not None else k_out
+    _check(
+        lib().itq3s_cache_append(
+            _ptr(q), _ld(q) if q is not None else 0, q_heads, _ptr(k), _ld(k) if k is not None else 0, _ptr(v), _ld(v) if v is not None else 0, T,
+            F16 if first.dtype == torch.float16 else F32, kv_heads, head_dim, _ptr(q_norm), _ptr(k_norm), eps, _ptr(positions), _ptr(freq), rot, interleaved, gain,
+            _ptr(q_out), _ld(q_out) if q_out is not None else 0, _ptr(k_out), _ld(k_out) if k_out is not None else 0,
+            F32 if out is not None and out.dtype == torch.float32 else F16, desc, _ptr(slots), _ptr(status_flags), _stream(),
+        )
+    )
+    return q_out, k_out
+
+
+def itq3s_cache_read(cache, slots, k_out=None, v_out=None, dtype=torch.float16, status_flags=None):
+    """Rows of the cache as the values that they stand for: (K, V) [T, kv_heads * head_dim], float16 or float32, of slots [T]
+    (int64; negative: zeros)."""
+    _need_here(cache.data, slots, k_out, v_out, status_flags)
+    desc = _need_cache(cache)
+    if slots.dim() != 1:
+        raise Itq3sError("slots must be a contiguous int64 tensor")
+    T, width = slots.shape[0], cache.kv_heads * cache.head_dim
+    _need_list("slots", slots, T, torch.int64)
+    if k_out is None:
+        k_out = torch.empty((T, width), dtype=v_out.dtype if v_out is not None else dtype, device=slots.device)
+    if v_out is None:
+        v_out = torch.empty((T, width), dtype=k_out.dtype, device=slots.device)
+    _need_rows("k_out", k_out, T, width, _FLOATS)
+    _need_rows("v_out", v_out, T, width, (k_out.dtype,))
+    _need_flags(status_flags)
+    _check(lib().itq3s_cache_read(desc, _ptr(slots), T, _ptr(k_out), _ld(k_out), _ptr(v_out), _ld(v_out), F16 if k_out.dtype == torch.float16 else F32, _ptr(status_flags), _stream()))
+    return k_out, v_out
+
+
+def itq3s_cache_attention_workspace_bytes(T, seqs, q_heads, kv_heads, head_dim, max_q, max_kv):
+    return lib().itq3s_cache_attention_workspace_bytes(T, seqs, q_heads, kv_heads, head_dim, max_q, max_kv)
+
+
+def itq3s_cache_attention(q, cache, q_starts, kv_lens, pages, scale=None, max_q=None, max_kv=None, out=None, workspace=None, status_flags=None):
+    """Attention of the last rows of every sequence over the cache, causal: q [T, q_heads * head_dim] float16, rows
+    q_starts[s] .. q_starts[s + 1] - 1 of sequence s, whose kv_lens[s] tokens (those rows' own among them) are in the pages
+    pages[s] (all int32, [seqs + 1], [seqs], [seqs, pages]).  -> out, as q.
+
+    scale: 1 / sqrt(head_dim) if not given; max_q, max_kv: the most rows and tokens of a sequence to cut the work up for (T and what the
+    page table has room for if not given); workspace: uint8, allocated here if not given."""
+    _need_here(q, cache.data, q_starts, kv_lens, pages, out, workspace, status_flags)
+    desc = _need_cache(cache)
+    if q.dim() != 2:
+        raise Itq3sError("q must be float16 [T, q_heads * head_dim] with unit column stride")
+    D = cache.head_dim
+    T, q_heads = q.shape[0], max(q.shape[1] // D, 1)
+    _need_rows("q", q, T, q_heads * D, _HALF)
+    if kv_lens.dim() != 1:
+        raise Itq3sError("kv_lens must be a contiguous int32 tensor")
+    seqs = kv_lens.shape[0]
+    _need_list("kv_lens", kv_lens, seqs, torch.int32)
+    _need_list("q_starts", q_starts, seqs + 1, torch.int32)
+    if pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] != seqs or pages.shape[1] < 1 or pages.stride(1) != 1 or (seqs > 1 and pages.stride(0) != pages.shape[1]):
+        raise Itq3sError("pages must be a contiguous int32 tensor [%d, pages]" % seqs)
+    if out is None:
+        out = torch.empty((T, q_heads * D), dtype=torch.float16, device=q.device)
+    _need_rows("out", out, T, q_heads * D, _HALF)
+    _need_flags(status_flags)
+    if max_q is None:
+        max_q = T
+    if max_kv is None:
+        max_kv = pages.shape[1] * cache.page_tokens
+    if workspace is None:
+        workspace = torch.empty(itq3s_cache_attention_workspace_bytes(T, seqs, q_heads, cache.kv_heads, D, max_q, max_kv), dtype=torch.uint8, device=q.device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise Itq3sError("workspace must be a contiguous uint8 tensor")
+    _check(
+        lib().itq3s_cache_attention(
+            _ptr(q), _ld(q), T, q_heads, desc, _ptr(q_starts), _ptr(kv_lens), seqs, _ptr(pages), pages.shape[1], max_q, max_kv, D**-0.5 if scale is None else scale,
+            _ptr(out), _ld(out), _ptr(workspace), workspace.numel(), _ptr(status_flags), _stream(),
+        )
+    )
+    return out
+
+
+def itq3s_prompt_attention(q, k, v, head_dim, starts, max_len=None, causal=True, scale=None, out=None):
+    """Attention of whole prompts over their own keys and values, float16: q [T, q_heads * head_dim], k and v
+    [T, kv_heads * head_dim], rows starts[s] .. starts[s + 1] - 1 of sequence s (int32 [seqs + 1]).  -> out, as q.
+
+    max_len: the most rows of a sequence to cut the work up for (T if not given); scale: 1 / sqrt(head_dim) if not given."""
+    _need_here(q, k, v, starts, out)
+    if head_dim not in (64, 128, 256):
+        raise Itq3sError("head_dim must be 64, 128 or 256")
+    if q.dim() != 2 or k.dim() != 2:
+        raise Itq3sError("q and k must be float16 [T, heads * head_dim] with unit column stride")
+    T, q_heads, kv_heads = q.shape[0], max(q.shape[1] // head_dim, 1), max(k.shape[1] // head_dim, 1)
+    _need_rows("q", q, T, q_heads * head_dim, _HALF)
+    _need_rows("k", k, T, kv_heads * head_dim, _HALF)
+    _need_rows("v", v, T, kv_heads * head_dim, _HALF)
+    if starts.dim() != 1 or starts.shape[0] < 2:
+        raise Itq3sError("starts must be a contiguous int32 tensor of at least two")
+    seqs = starts.shape[0] - 1
+    _need_list("starts", starts, seqs + 1, torch.int32)
+    if out is None:
+        out = torch.empty((T, q_heads * head_dim), dtype=torch.float16, device=q.device)
+    _need_rows("out", out, T, q_heads * head_dim, _HALF)
+    _check(
+        lib().itq3s_prompt_attention(
+            _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), T, q_heads, kv_heads, head_dim, _ptr(starts), seqs, T if max_len is None else max_len, causal,
+            head_dim**-0.5 if scale is None else scale, _ptr(out), _ld(out), _stream(),
+        )
+    )
     return out

@@ -1,0 +1,472 @@
+// Norm and position rotation of query and key heads, keys and values into the 4-bit cache, and back.
+//
+// A row is one head of one token, D values x.  Norm: x w / sqrt(mean x^2 + eps).  Rotation: pairs (a, b) of channels turn by
+// the angle position * freq[i]: (a cos - b sin, b cos + a sin), times a gain.  Cache: w = H x with the orthonormal
+// Walsh-Hadamard matrix of D points, step s = max|w| / 7.5 rounded to fp16, digit c = floor(w / s + 1/2) within -8..7;
+// the row stands for H (s c).  The transform spreads an outlier channel over the row, so that one step serves it whole.
+//
+// What decides digits is computed in 64 bits (keys and values; the vector ALU issues a 64-bit addition at the rate of an
+// unpacked 32-bit one), so that a digit depends on the definition alone and not on an order of summation or on a
+// library's sine: with 32 bits some 1e-6 of the digits fall on the other side of their border.  Queries, which are
+// only rounded, take 32 bits behind a 64-bit angle.
+//
+// A lane holds eight channels of a row: 8, 16 or 32 lanes a row, 8, 4 or 2 rows a wavefront, the rows of one wavefront
+// neighbouring tokens (so that their value bytes share words of memory) or, where there are few tokens, heads of a token.
+// It computes the sines of its channels once and walks over heads with them.  Everything is bound by memory: append
+// moves 2 or 4 bytes a value in and out, read 4.1 bits in and 2 or 4 bytes out.
+#include <type_traits>
+
+#include "itq3s_attention.h"
+#include "itq3s_cache.h"
+
+namespace itq3s {
+
+namespace {
+
+// eight neighbouring values
+__device__ __forceinline__ void load8(const _Float16* p, _Float16 (&v)[8]) {
+    const half8 h = *reinterpret_cast<const half8*>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = h[j];
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const floatx4 a = reinterpret_cast<const floatx4*>(p)[0], b = reinterpret_cast<const floatx4*>(p)[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+}
+template <typename R>
+__device__ __forceinline__ void store8(_Float16* p, const R (&v)[8]) {
+    half8 h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (_Float16)(float)v[j];  // 64 bits by way of 32, as everywhere in the library
+    *reinterpret_cast<half8*>(p) = h;
+}
+template <typename R>
+__device__ __forceinline__ void store8(float* p, const R (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) reinterpret_cast<floatx4*>(p)[i] = floatx4{(float)v[4 * i], (float)v[4 * i + 1], (float)v[4 * i + 2], (float)v[4 * i + 3]};
+}
+
+__device__ __forceinline__ float xor_lane(float v, int m) { return xor_lane_f32(v, m); }
+__device__ __forceinline__ double xor_lane(double v, int m) { return xor_lane_f64(v, m); }
+
+// sine and cosine in 64 bits: the angle less the nearest multiple of pi/2 (pi/2 in two parts, products by fused
+// multiply-add: exact to 1e-17 for the 2^31 positions there are), then the Taylor series, whose first left-out terms are
+// (pi/4)^19 / 19! = 8e-20 and (pi/4)^18 / 18! = 2e-18.
+__device__ __forceinline__ void turn(double angle, double& c, double& s) {
+    const double n = __builtin_rint(angle * 0.63661977236758134308);
+    double r = __builtin_fma(n, -1.5707963267948965580, angle);
+    r = __builtin_fma(n, -6.1232339957367660359e-17, r);
+    const double z = r * r;
+    double a = 1.0 / 355687428096000.0, b = 1.0 / 20922789888000.0;  // 17!, 16!
+    a = __builtin_fma(a, z, -1.0 / 1307674368000.0), b = __builtin_fma(b, z, -1.0 / 87178291200.0);
+    a = __builtin_fma(a, z, 1.0 / 6227020800.0), b = __builtin_fma(b, z, 1.0 / 479001600.0);
+    a = __builtin_fma(a, z, -1.0 / 39916800.0), b = __builtin_fma(b, z, -1.0 / 3628800.0);
+    a = __builtin_fma(a, z, 1.0 / 362880.0), b = __builtin_fma(b, z, 1.0 / 40320.0);
+    a = __builtin_fma(a, z, -1.0 / 5040.0), b = __builtin_fma(b, z, -1.0 / 720.0);
+    a = __builtin_fma(a, z, 1.0 / 120.0), b = __builtin_fma(b, z, 1.0 / 24.0);
+    a = __builtin_fma(a, z, -1.0 / 6.0), b = __builtin_fma(b, z, -0.5);
+    const double sn = __builtin_fma(r * z, a, r), cs = __builtin_fma(z, b, 1.0);
+    const int q = (int)__builtin_fma(-4.0, __builtin_floor(n * 0.25), n);
+    s = (q & 1) ? cs : sn;
+    c = (q & 1) ? sn : cs;
+    if (q & 2) s = -s;
+    if ((q + 1) & 2) c = -c;
+}
+
+struct AppendArgs {
+    const void *Q, *K, *V;
+    void *Q_out, *K_out;
+    const float *q_norm, *k_norm;
+    const int32_t* positions;
+    const double* freq;
+    unsigned char* data;
+    const int64_t* slots;
+    uint32_t* flags;
+    int64_t ldq, ldk, ldv, ldqo, ldko, T, slots_end;
+    int q_heads, kv_heads, rot, interleaved;
+    float eps, gain;
+    int page_blocks;                  // blocks of 32 tokens a page
+    int tokens;                       // neighbouring tokens in a wavefront (1 or as many as it has rows)
+    int q_step, kv_step;              // heads that a wavefront walks over
+    int64_t groups;                   // token groups
+    int64_t k_jobs, v_jobs, q_jobs;   // wavefronts
+};
+
+template <int D>
+struct Rows {
+    static constexpr int kLanes = D / 8, kRows = 64 / kLanes;
+    __device__ static __forceinline__ int row() { return lane_id() / kLanes; }
+    __device__ static __forceinline__ int channel() { return lane_id() % kLanes * 8; }
+};
+
+// Sines and cosines of a lane's channels (pairs of channels where they are interleaved), gain and sign of the sine in.
+template <typename R>
+struct Turns {
+    R c[8], s[8];
+};
+template <typename R>
+__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, int ch, Turns<R>& t) {
+    const double pos = (double)a.positions[token], gain = (double)a.gain;
+    const int half = a.rot / 2;
+    const bool upper = ch >= half;
+    double c = 0.0, s = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (j % 2 == 0 || !a.interleaved) turn(pos * a.freq[a.interleaved ? (ch + j) / 2 : (upper ? ch - half : ch) + j], c, s);
+        const bool second = a.interleaved ? j % 2 == 1 : upper;  // of its pair
+        t.c[j] = (R)(c * gain);
+        t.s[j] = (R)((second ? s : -s) * gain);
+    }
+}
+
+// One row through norm and rotation.
+template <int D, typename R, typename In>
+__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const In (&x)[8], const float (&w)[8], const float (&wp)[8], bool normed, bool turned, int partner,
+                                              const Turns<R>& t, R (&y)[8]) {
+    R f = (R)1;
+    if (normed) {
+        R sum = (R)0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = sum + (R)x[j] * (R)x[j];
+#pragma unroll
+        for (int m = 1; m < Rows<D>::kLanes; m *= 2) sum = sum + xor_lane(sum, m);
+        f = (R)1 / __builtin_elementwise_sqrt(sum * (R)(1.0 / D) + (R)a.eps);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = normed ? (R)x[j] * f * (R)w[j] : (R)x[j];
+    if (a.rot == 0) return;
+    R other[8];
+    if (a.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) other[j] = y[j ^ 1];
+    } else {  // the partner's eight channels are another lane's: its values as they came, the norm's factor is the row's
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (std::is_same<In, _Float16>::value) {
+                // two values a word
+                if (j % 2 == 0) {
+                    const uint32_t mine = (uint32_t)__builtin_bit_cast(uint16_t, x[j]) | (uint32_t)__builtin_bit_cast(uint16_t, x[j + 1]) << 16;
+                    const uint32_t got = (uint32_t)__shfl((int)mine, partner, 64);
+                    other[j] = (R)__builtin_bit_cast(_Float16, (uint16_t)got);
+                    other[j + 1] = (R)__builtin_bit_cast(_Float16, (uint16_t)(got >> 16));
+                }
+            } else {
+                other[j] = (R)__shfl(x[j], partner, 64);
+            }
+        }
+        if (normed) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) other[j] = other[j] * f * (R)wp[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (turned) y[j] = y[j] * t.c[j] + other[j] * t.s[j];
+}
+
+// One row into the cache: transform, step, digits.  Rows without a slot do everything but the stores.
+template <int D>
+__device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8], int64_t slot, bool live, int head, bool is_value) {
+    hadamard<D>(v);
+    double most = 0.0;
+    bool finite = true;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        finite = finite && __builtin_fabs(v[j]) <= 1.7976931348623157e308;
+        most = __builtin_fmax(most, __builtin_fabs(v[j]));
+    }
+#pragma unroll
+    for (int m = 1; m < Rows<D>::kLanes; m *= 2) most = __builtin_fmax(most, xor_lane_f64(most, m));
+    int bad = finite ? 0 : 1;
+#pragma unroll
+    for (int m = 1; m < Rows<D>::kLanes; m *= 2) bad |= xor_lane_i32(bad, m);
+    const float s32 = (float)(most * (1.0 / (7.5 * kRootD<D>)));
+    const bool sat = s32 > 65504.f;
+    _Float16 s = (_Float16)(sat ? 65504.f : s32);
+    if (bad) s = (_Float16)0.f;
+    const double step = (double)(float)s * kRootD<D>, inv = step > 0.0 ? 1.0 / step : 0.0;
+    int d[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // floor(w / step + 1/2): by the reciprocal, then set right by the remainder, whose sign is exact
+        double q = __builtin_floor(__builtin_fma(v[j], inv, 0.5));
+        const double rest = __builtin_fma(-q, step, v[j]);
+        if (rest >= 0.5 * step) q += 1.0;
+        if (rest < -0.5 * step) q -= 1.0;
+        q = __builtin_fmin(__builtin_fmax(q, -8.0), 7.0);
+        d[j] = step > 0.0 ? (int)q + 8 : 8;
+    }
+    const int lane = lane_id(), ch = Rows<D>::channel();
+    if (a.flags != nullptr && live && ch == 0 && (bad || sat)) atomicOr(a.flags, bad ? kFlagNonFinite : kFlagScaleSat);
+    const int t = (int)(slot & 31);
+    const int64_t block = slot >> 5;
+    unsigned char* const base = a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks));
+    if (!is_value) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w |= (uint32_t)d[j] << (4 * ((j >> 1) + 4 * (j & 1)));
+        if (live) *reinterpret_cast<uint32_t*>(base + t * (D / 2) + ch / 2) = w;
+    } else {
+        // channels c and c + 16 of a group of 32 share a byte: lanes l and l ^ 2 hold them, each makes four of the bytes
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w |= (uint32_t)d[j] << (4 * j);
+        const uint32_t o = (uint32_t)row_xor_i32<2>((int)w);
+        const bool upper = (lane & 2) != 0;
+        const uint32_t lo = upper ? o >> 16 : w, hi = upper ? w >> 16 : o;
+        const int p = ch / 32, c = (ch & 8) + (upper ? 4 : 0);
+        unsigned char* const at = base + 16 * D + value_byte(t, p, c);
+        if (live) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) at[16 * j] = (unsigned char)(((lo >> (4 * j)) & 15u) | ((hi >> (4 * j)) & 15u) << 4);
+        }
+    }
+    if (live && ch == 0) *reinterpret_cast<_Float16*>(base + 32 * D + 4 * t + (is_value ? 2 : 0)) = s;
+}
+
+// One wavefront: its token group's rows for heads h0 .. h1 - 1 of the queries (what 0), the keys (1) or the values (2).
+template <int D, typename In, typename Out, int kWhat>
+__device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, int h0, int h1) {
+    typedef typename std::conditional<kWhat == 0, float, double>::type R;
+    const int row = Rows<D>::row(), ch = Rows<D>::channel();
+    const bool by_token = a.tokens > 1;
+    const int64_t token = by_token ? group * Rows<D>::kRows + row : group;
+    const bool here = token < a.T;
+    const int64_t tok = here ? token : a.T - 1;
+    const int64_t ld = kWhat == 0 ? a.ldq : kWhat == 1 ? a.ldk : a.ldv;
+    const In* const src = static_cast<const In*>(kWhat == 0 ? a.Q : kWhat == 1 ? a.K : a.V) + tok * ld + ch;
+    Out* const dst = kWhat == 2 ? nullptr : static_cast<Out*>(kWhat == 0 ? a.Q_out : a.K_out);
+    const int64_t ldo = kWhat == 0 ? a.ldqo : a.ldko;
+    const bool cached = kWhat != 0 && a.data != nullptr;
+    int64_t slot = 0;
+    bool live = false;
+    if (cached) {
+        slot = a.slots[tok];
+        live = here && slot >= 0 && slot < a.slots_end;
+        if (here && slot >= a.slots_end && ch == 0 && a.flags != nullptr) atomicOr(a.flags, kFlagBadSlot);
+        if (!live) slot = 0;
+    }
+    Turns<R> t;
+    float w[8], wp[8];
+    const int half = a.rot / 2, pch = ch < half ? ch + half : ch - half;
+    const bool turned = kWhat != 2 && ch < a.rot;
+    const int partner = lane_id() + (turned ? pch - ch : 0) / 8;
+    const float* const norm = kWhat == 0 ? a.q_norm : kWhat == 1 ? a.k_norm : nullptr;
+    if constexpr (kWhat != 2) {
+        if (turned) find_turns<R>(a, tok, ch, t);
+        if (norm != nullptr) {
+            load8(norm + ch, w);
+            load8(norm + (turned ? pch : ch), wp);
+        }
+    }
+    const int step = by_token ? 1 : Rows<D>::kRows;
+    const int heads = kWhat == 0 ? a.q_heads : a.kv_heads;
+    In x[8];
+    {
+        const int h = by_token ? h0 : h0 + row;
+        load8(src + (int64_t)(h < heads ? h : heads - 1) * D, x);
+    }
+    for (int hb = h0; hb < h1; hb += step) {
+        const int h = by_token ? hb : hb + row;
+        In next[8];
+        const int hn = h + step;
+        load8(src + (int64_t)(hn < heads ? hn : heads - 1) * D, next);
+        R y[8];
+        if constexpr (kWhat == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (R)x[j];
+        } else {
+            norm_and_turn<D>(a, x, w, wp, norm != nullptr, turned, partner, t, y);
+            if (dst != nullptr && here && h < h1) store8(dst + tok * ldo + (int64_t)h * D + ch, y);
+        }
+        if constexpr (kWhat != 0) {
+            if (cached) quantize_row<D>(a, y, slot, live && h < h1, h < heads ? h : 0, kWhat == 2);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = next[j];
+    }
+}
+
+template <int D, typename In, typename Out>
+__global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
+    int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (job < a.k_jobs) {
+        const int h0 = (int)(job / a.groups) * a.kv_step;
+        append_rows<D, In, Out, 1>(a, job % a.groups, h0, h0 + a.kv_step < a.kv_heads ? h0 + a.kv_step : a.kv_heads);
+        return;
+    }
+    job -= a.k_jobs;
+    if (job < a.v_jobs) {
+        const int h0 = (int)(job / a.groups) * a.kv_step;
+        append_rows<D, In, Out, 2>(a, job % a.groups, h0, h0 + a.kv_step < a.kv_heads ? h0 + a.kv_step : a.kv_heads);
+        return;
+    }
+    job -= a.v_jobs;
+    if (job < a.q_jobs) {
+        const int h0 = (int)(job / a.groups) * a.q_step;
+        append_rows<D, In, Out, 0>(a, job % a.groups, h0, h0 + a.q_step < a.q_heads ? h0 + a.q_step : a.q_heads);
+    }
+}
+
+// ---- read
+
+struct ReadArgs {
+    const unsigned char* data;
+    const int64_t* slots;
+    void *K, *V;
+    uint32_t* flags;
+    int64_t ldk, ldv, T, slots_end;
+    int kv_heads, page_blocks;
+};
+
+// The transform of a row of digits: sums of at most 256 * 8 = 2^11 in fp16, so every step is exact.  Pairs (2i, 2i + 1).
+template <int D>
+__device__ __forceinline__ void hadamard_digits(half2v (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = half2v{v[i][0], v[i][0]} + half2v{v[i][1], -v[i][1]};
+#pragma unroll
+    for (int h = 1; h < 4; h *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((i & h) == 0) {
+                const half2v a = v[i], b = v[i + h];
+                v[i] = a + b;
+                v[i + h] = a - b;
+            }
+    const int lane = lane_id();
+#define ITQ3S_STAGE(m)                                                                                                    \
+    if constexpr ((m) < D / 8) {                                                                                          \
+        const _Float16 sign = (lane & (m)) != 0 ? (_Float16)-1.f : (_Float16)1.f;                                         \
+        _Pragma("unroll") for (int i = 0; i < 4; ++i)                                                                     \
+            v[i] = half2v{sign, sign} * v[i] + __builtin_bit_cast(half2v, row_xor_i32<(m)>(__builtin_bit_cast(int, v[i]))); \
+    }
+    ITQ3S_STAGE(1) ITQ3S_STAGE(2) ITQ3S_STAGE(4) ITQ3S_STAGE(8) ITQ3S_STAGE(16)
+#undef ITQ3S_STAGE
+}
+
+// A workgroup reads 32 listed rows of one head.  Key words go straight to their lanes; value bytes, which lie eight tokens
+// beside each other, are gathered token-fastest (neighbouring slots: neighbouring bytes) and turned round in LDS.
+template <int D, typename Out>
+__global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
+    constexpr int kRows = Rows<D>::kRows, kPitch = D / 2 + 8;
+    __shared__ __align__(16) unsigned char turn_round[32 * kPitch];
+    const int head = blockIdx.y;
+    const int64_t first = (int64_t)blockIdx.x * 32;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    {
+        const int i = tid & 31;
+        const int64_t token = first + i;
+        int64_t slot = token < a.T ? a.slots[token] : -1;
+        const bool live = slot >= 0 && slot < a.slots_end;
+        if (slot >= a.slots_end && tid < 32 && head == 0 && a.flags != nullptr) atomicOr(a.flags, kFlagBadSlot);
+        if (!live) slot = 0;
+        const int64_t block = slot >> 5;
+        const unsigned char* const at = a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks)) + 16 * D;
+        const int t = (int)(slot & 31);
+        unsigned char got[D / 16];
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const int b = (tid >> 5) + 8 * k;  // byte p * 16 + c of the token
+            got[k] = at[value_byte(t, b >> 4, b & 15)];
+        }
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) turn_round[i * kPitch + (tid >> 5) + 8 * k] = got[k];
+    }
+    __syncthreads();
+    const int row = Rows<D>::row(), ch = Rows<D>::channel();
+#pragma unroll
+    for (int r0 = 0; r0 < 8; r0 += kRows) {
+        const int i = wave * 8 + r0 + row;
+        const int64_t token = first + i;
+        const bool here = token < a.T;
+        int64_t slot = here ? a.slots[token] : -1;
+        const bool live = slot >= 0 && slot < a.slots_end;
+        if (!live) slot = 0;
+        const int t = (int)(slot & 31);
+        const int64_t block = slot >> 5;
+        const unsigned char* const base = a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks));
+        const uint32_t kw = *reinterpret_cast<const uint32_t*>(base + t * (D / 2) + ch / 2);
+        const uint32_t steps = *reinterpret_cast<const uint32_t*>(base + 32 * D + 4 * t);
+        const u32x2 vb = *reinterpret_cast<const u32x2*>(turn_round + i * kPitch + (ch / 32) * 16 + (ch & 8));
+        const int shift = (ch & 16) != 0 ? 4 : 0;
+        half2v k[4] = {low_pair(kw), high_pair(kw), low_pair(kw >> 8), high_pair(kw >> 8)};
+        half2v v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t w = vb[j >> 1] >> ((j & 1) * 16 + shift);
+            v[j] = low_pair((w & 15u) | ((w & 0x0f00u) << 8));
+        }
+        hadamard_digits<D>(k);
+        hadamard_digits<D>(v);
+        const float root = (float)(1.0 / kRootD<D>);
+        const float ks = live ? f16_bits_to_f32(steps & 0xffffu) * root : 0.f, vs = live ? f16_bits_to_f32(steps >> 16) * root : 0.f;
+        if (here) {
+            float kf[8], vf[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kf[j] = live ? (float)k[j >> 1][j & 1] * ks : 0.f, vf[j] = live ? (float)v[j >> 1][j & 1] * vs : 0.f;
+            store8(static_cast<Out*>(a.K) + token * a.ldk + (int64_t)head * D + ch, kf);
+            store8(static_cast<Out*>(a.V) + token * a.ldv + (int64_t)head * D + ch, vf);
+        }
+    }
+}
+
+template <int D, typename In, typename Out>
+int start_append(const AppendArgs& a, int64_t blocks, hipStream_t st) {
+    append_kernel<D, In, Out><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
+    return hipGetLastError() == hipSuccess ? 0 : -6;
+}
+template <int D>
+int start_append(const AppendArgs& a, int64_t blocks, int in_f16, int out_f16, hipStream_t st) {
+    if (in_f16) return out_f16 ? start_append<D, _Float16, _Float16>(a, blocks, st) : start_append<D, _Float16, float>(a, blocks, st);
+    return out_f16 ? start_append<D, float, _Float16>(a, blocks, st) : start_append<D, float, float>(a, blocks, st);
+}
+
+}  // namespace
+
+int launch_append(const AppendCall& c, hipStream_t st) {
+    const int rows = 512 / c.head_dim;  // of a wavefront
+    AppendArgs a{};
+    a.Q = c.Q, a.K = c.K, a.V = c.V, a.Q_out = c.Q_out, a.K_out = c.K_out;
+    a.q_norm = c.q_norm, a.k_norm = c.k_norm, a.positions = c.positions, a.freq = c.freq, a.slots = c.slots, a.flags = c.flags;
+    a.ldq = c.ldq, a.ldk = c.ldk, a.ldv = c.ldv, a.ldqo = c.ldqo, a.ldko = c.ldko, a.T = c.T;
+    a.q_heads = c.Q != nullptr ? c.q_heads : 0, a.kv_heads = c.kv_heads, a.rot = c.rot, a.interleaved = c.interleaved, a.eps = c.eps, a.gain = c.gain;
+    a.data = c.cache.data, a.page_blocks = c.cache.data != nullptr ? c.cache.page_blocks : 1;
+    a.slots_end = c.cache.data != nullptr ? c.cache.pages * c.cache.page_blocks * kCacheBlock : 0;
+    // Neighbouring tokens in a wavefront where that leaves every compute unit four of them, else heads of one token.
+    a.tokens = c.T * c.kv_heads / rows >= 4 * (int64_t)cu_count() ? rows : 1;
+    a.groups = (c.T + a.tokens - 1) / a.tokens;
+    // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  16 a unit are plenty.
+    auto heads_of = [&](int heads) {
+        int step = a.tokens > 1 ? 1 : rows;
+        while (step < heads && a.groups * ((heads + 2 * step - 1) / (2 * step)) >= 16 * (int64_t)cu_count()) step *= 2;
+        return step;
+    };
+    a.q_step = heads_of(a.q_heads), a.kv_step = heads_of(c.kv_heads);
+    a.k_jobs = c.K != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
+    a.v_jobs = c.V != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
+    a.q_jobs = a.q_heads > 0 ? a.groups * ((a.q_heads + a.q_step - 1) / a.q_step) : 0;
+    const int64_t blocks = (a.k_jobs + a.v_jobs + a.q_jobs + 3) / 4;
+    if (blocks > 0x7fffffffLL) return -2;
+    if (c.head_dim == 64) return start_append<64>(a, blocks, c.in_f16, c.out_f16, st);
+    if (c.head_dim == 128) return start_append<128>(a, blocks, c.in_f16, c.out_f16, st);
+    return start_append<256>(a, blocks, c.in_f16, c.out_f16, st);
+}
+
+int launch_cache_read(const CacheView& cache, const int64_t* slots, int64_t T, void* K, int64_t ldk, void* V, int64_t ldv, int out_f16, uint32_t* flags, hipStream_t st) {
+    const ReadArgs a{cache.data, slots, K, V, flags, ldk, ldv, T, cache.pages * cache.page_blocks * kCacheBlock, cache.kv_heads, cache.page_blocks};
+    const dim3 grid((unsigned)((T + 31) / 32), (unsigned)cache.kv_heads);
+    if (cache.head_dim == 64) {
+        if (out_f16) read_kernel<64, _Float16><<<grid, dim3(256), 0, st>>>(a);
+        else read_kernel<64, float><<<grid, dim3(256), 0, st>>>(a);
+    } else if (cache.head_dim == 128) {
+        if (out_f16) read_kernel<128, _Float16><<<grid, dim3(256), 0, st>>>(a);
+        else read_kernel<128, float><<<grid, dim3(256), 0, st>>>(a);
+    } else {
+        if (out_f16) read_kernel<256, _Float16><<<grid, dim3(256), 0, st>>>(a);
+        else read_kernel<256, float><<<grid, dim3(256), 0, st>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? 0 : -6;
+}
+
+}  // namespace itq3s

@@ -1,0 +1,223 @@
+// Attention of whole prompts over their own keys and values in fp16: o = softmax(scale q k^T) v, causal or not, grouped
+// heads, sequences of different lengths packed behind each other.
+//
+// A wavefront takes 32 or 64 query rows (a row: one head of one token; the heads of a group are neighbouring rows, so that a
+// workgroup's keys serve them all) as columns of  S^T = K Q^T  and  O^T += V^T P^T.  With 32x32x16 products the accumulator of
+// S^T leaves a lane, for its column, the tokens 16 k + 4 (l / 32) + {0..3, 8..11} of step k: taken as they stand they are the
+// operand P^T of step k, if V^T comes with its tokens in the same order.  So weights never leave their lane, and only a
+// row's maximum crosses to one other lane, when it moves by more than 2^8 (else the old reference is as good).
+// Keys and values pass through LDS in tiles of 64 tokens, rows as in memory, 16-byte chunks permuted within a row
+// against bank conflicts; V^T is read with the transposing LDS read.  The next tile is on its way to registers meanwhile.
+#include "itq3s_attention.h"
+#include "itq3s_cache.h"
+
+namespace itq3s {
+
+namespace {
+
+constexpr float kNoRow = -1e30f;
+constexpr float kHeadroom = 8.f;
+template <int D>
+constexpr int kTile = D <= 128 ? 64 : 32;  // tokens of a tile
+
+struct PromptArgs {
+    const _Float16 *Q, *K, *V;
+    const int32_t* starts;
+    _Float16* out;
+    int64_t ldq, ldk, ldv, ldo, T;
+    float scale;    // |softmax scale| * log2(e)
+    _Float16 sign;  // the scale's sign, which the queries take (a scale of 0: 0, and any other scale)
+    int q_heads, kv_heads, group, seqs, tiles, causal;
+};
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ half4 read_turned(const _Float16* p) {
+    typedef __attribute__((address_space(3))) short4v* lds_t;
+    return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(short4v*)p));
+}
+
+// Where chunk c (eight channels) of row r of a tile stands: keys are read a row a lane, so rows shift by one; values four
+// rows of two chunks at once, so rows shift by two.
+template <int D>
+__device__ __forceinline__ int k_at(int r, int c) { return (r * (D / 8) + (c ^ (r & (D / 8 < 16 ? D / 8 - 1 : 15)))) * 8; }
+template <int D>
+__device__ __forceinline__ int v_at(int r, int c) { return (r * (D / 8) + (c ^ ((2 * r) & (D / 8 < 16 ? D / 8 - 1 : 15)))) * 8; }
+
+template <int D, int RT>
+__global__ void __launch_bounds__(256) prompt_kernel(const PromptArgs a) {
+    constexpr int kChunks = kTile<D> * D / 8 / 256;  // 16-byte chunks of a tile a thread moves
+    __shared__ __align__(16) _Float16 ks[kTile<D> * D];
+    __shared__ __align__(16) _Float16 vs[kTile<D> * D];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = lane_id(), hi = lane >> 5, col = lane & 31;
+    int id = blockIdx.x;
+    const int head = id % a.kv_heads;
+    id /= a.kv_heads;
+    const int seq = id % a.seqs;
+    int64_t first = a.starts[seq], end = a.starts[seq + 1];
+    first = first < 0 ? 0 : first > a.T ? a.T : first;
+    end = end < first ? first : end > a.T ? a.T : end;
+    const int len = (int)(end - first), total = len * a.group;
+    constexpr int kRows = 128 * RT;
+    const int count = (total + kRows - 1) / kRows;
+    const _Float16* const kb = a.K + first * a.ldk + (int64_t)head * D;
+    const _Float16* const vb = a.V + first * a.ldv + (int64_t)head * D;
+    // the last rows have the most to see: they begin
+    for (int tile = count - 1 - id / a.seqs; tile >= 0; tile -= a.tiles) {
+        const int row0 = tile * kRows + wave * 32 * RT;
+        half8 q[RT][D / 16];
+        int see[RT];
+        floatx16 o[D / 32][RT];
+        float m[RT], l[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int row = row0 + 32 * t + col;
+            const bool there = row < total;
+            const int i = there ? row / a.group : 0, hq = head * a.group + (there ? row % a.group : 0);
+            const half8* const p = reinterpret_cast<const half8*>(a.Q + (first + i) * a.ldq + (int64_t)hq * D + 8 * hi);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) q[t][k] = there ? p[2 * k] * a.sign : half8{};
+            see[t] = !there ? 0 : a.causal ? i + 1 : len;
+            m[t] = kNoRow, l[t] = 0.f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[c][t][x] = 0.f;
+        }
+        const int last_row = (tile + 1) * kRows < total ? (tile + 1) * kRows - 1 : total - 1;
+        const int tokens = a.causal ? last_row / a.group + 1 : len;  // that the workgroup needs
+        const int my_last = row0 + 32 * RT < total ? row0 + 32 * RT - 1 : total - 1;
+        const int mine = row0 >= total ? 0 : a.causal ? my_last / a.group + 1 : len;  // that this wavefront needs
+        const int all = row0 >= total ? 0 : a.causal ? row0 / a.group + 1 : len;      // that all of its rows see
+
+        half8 kr[kChunks], vr[kChunks];
+        auto load = [&](int t0) {
+#pragma unroll
+            for (int u = 0; u < kChunks; ++u) {
+                const int x = tid + 256 * u, r = t0 + x / (D / 8), c = x % (D / 8);
+                const bool in = r < len;  // rows behind the sequence are another's, or nothing: zeros
+                const int64_t rr = in ? r : len - 1;
+                kr[u] = *reinterpret_cast<const half8*>(kb + rr * a.ldk + 8 * c);
+                vr[u] = *reinterpret_cast<const half8*>(vb + rr * a.ldv + 8 * c);
+                if (!in) kr[u] = half8{}, vr[u] = half8{};
+            }
+        };
+        load(0);
+        for (int t0 = 0; t0 < tokens; t0 += kTile<D>) {
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kChunks; ++u) {
+                const int x = tid + 256 * u, r = x / (D / 8), c = x % (D / 8);
+                *reinterpret_cast<half8*>(ks + k_at<D>(r, c)) = kr[u];
+                *reinterpret_cast<half8*>(vs + v_at<D>(r, c)) = vr[u];
+            }
+            __syncthreads();
+            if (t0 + kTile<D> < tokens) load(t0 + kTile<D>);
+            if (t0 >= mine) continue;
+#pragma unroll
+            for (int tt = 0; tt < kTile<D> / 32; ++tt) {
+                floatx16 s[RT];
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[t][x] = 0.f;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const half8 kf = *reinterpret_cast<const half8*>(ks + k_at<D>(32 * tt + col, 2 * k + hi));
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[t][k], s[t], 0, 0, 0);
+                }
+                half8 p[RT][2];
+                const bool edge = t0 + 32 * tt + 32 > all;
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if (edge) {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            s[t][x] = t0 + 32 * tt + 8 * (x / 4) + 4 * hi + x % 4 < see[t] ? s[t][x] : -__builtin_inff();
+                    }
+                    float top = s[t][0];
+#pragma unroll
+                    for (int x = 1; x < 16; ++x) top = __builtin_fmaxf(top, s[t][x]);
+                    top *= a.scale;
+                    if (__builtin_amdgcn_ballot_w64(top > m[t] + kHeadroom) != 0) {
+                        top = __builtin_fmaxf(top, xor_lane_f32(top, 32));
+                        const float n = __builtin_fmaxf(m[t], top), f = __builtin_amdgcn_exp2f(m[t] - n);
+                        m[t] = n;
+                        l[t] *= f;
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) o[c][t][x] *= f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][x], a.scale, -m[t]));
+                        l[t] += e;
+                        p[t][x / 8][x % 8] = (_Float16)e;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        const int r = 32 * tt + 16 * k + 4 * hi + ((lane >> 2) & 3), ch = 32 * c + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                        const half4 u = read_turned(vs + v_at<D>(r, ch / 8) + (ch & 4)), w = read_turned(vs + v_at<D>(r + 8, ch / 8) + (ch & 4));
+                        const half8 vf = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) o[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[t][k], o[c][t], 0, 0, 0);
+                    }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            l[t] += xor_lane_f32(l[t], 32);
+            const float f = l[t] == 0.f ? 0.f : 1.f / l[t];
+            const int row = row0 + 32 * t + col;
+            if (row < total) {
+                _Float16* const out = a.out + (first + row / a.group) * a.ldo + (int64_t)(head * a.group + row % a.group) * D + 4 * hi;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        *reinterpret_cast<half4*>(out + 32 * c + 8 * x) = half4{(_Float16)(o[c][t][4 * x] * f), (_Float16)(o[c][t][4 * x + 1] * f), (_Float16)(o[c][t][4 * x + 2] * f),
+                                                                                (_Float16)(o[c][t][4 * x + 3] * f)};
+            }
+        }
+    }
+}
+
+template <int D>
+int start(const PromptArgs& a, int64_t max_len, hipStream_t st) {
+    // 64 rows a wavefront where that leaves every compute unit a workgroup, else 32
+    const int64_t rows = max_len * a.group, units = (int64_t)a.seqs * a.kv_heads;
+    const bool wide = D <= 128 && units * ((rows + 255) / 256) >= cu_count();
+    PromptArgs b = a;
+    const int64_t per = wide ? 256 : 128, tiles = (rows + per - 1) / per;
+    if (units * tiles > 0x7fffffffLL) return -2;
+    b.tiles = (int)tiles;
+    const dim3 grid((unsigned)(units * tiles));
+    if constexpr (D <= 128) {
+        if (wide) {
+            prompt_kernel<D, 2><<<grid, dim3(256), 0, st>>>(b);
+            return hipGetLastError() == hipSuccess ? 0 : -6;
+        }
+    }
+    prompt_kernel<D, 1><<<grid, dim3(256), 0, st>>>(b);
+    return hipGetLastError() == hipSuccess ? 0 : -6;
+}
+
+}  // namespace
+
+int launch_prompt_attention(const PromptCall& c, hipStream_t st) {
+    PromptArgs a{};
+    a.Q = c.Q, a.K = c.K, a.V = c.V, a.starts = c.starts, a.out = c.out;
+    a.ldq = c.ldq, a.ldk = c.ldk, a.ldv = c.ldv, a.ldo = c.ldo, a.T = c.T;
+    a.scale = c.scale == 0.f ? 1.f : (float)(__builtin_fabs((double)c.scale) * 1.44269504088896340736);
+    a.sign = (_Float16)(c.scale > 0.f ? 1.f : c.scale < 0.f ? -1.f : 0.f);
+    a.q_heads = c.q_heads, a.kv_heads = c.kv_heads, a.group = c.q_heads / c.kv_heads, a.seqs = (int)c.seqs, a.causal = c.causal;
+    if (c.head_dim == 64) return start<64>(a, c.max_len, st);
+    if (c.head_dim == 128) return start<128>(a, c.max_len, st);
+    return start<256>(a, c.max_len, st);
+}
+
+}  // namespace itq3s
