@@ -308,7 +308,7 @@ int itq3s_cache_read(const itq3s_cache *cache, const int64_t *slots, int64_t T, 
  *            the cache is taken for tokens that nobody sees, ITQ3S_FLAG_BAD_SLOT; entries behind a sequence's last token are not read
  *   max_q, max_kv  the most rows and tokens of a sequence that the work is cut up for.  Longer sequences are computed all the same,
  *            slower; with max_q above T, T is meant
- *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  scale finite
+ *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  |scale| up to 2^40
  *   workspace device, 256-byte aligned, itq3s_cache_attention_workspace_bytes() of the same sizes (never 0); as for itq3s_matmul */
 size_t itq3s_cache_attention_workspace_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv);
 int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, const itq3s_cache *cache, const int32_t *q_starts,
@@ -322,7 +322,7 @@ int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, co
  *   Q, out T x (q_heads * head_dim), K, V T x (kv_heads * head_dim), all fp16;  out must not overlap the inputs
  *   starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it)
  *   max_len  the most rows of a sequence that the work is cut up for (longer ones are computed all the same, slower)
- *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  scale finite;  no workspace */
+ *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  |scale| up to 2^40;  no workspace */
 int itq3s_prompt_attention(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int q_heads,
                            int kv_heads, int head_dim, const int32_t *starts, int64_t seqs, int64_t max_len, int causal, float scale,
                            void *out, int64_t ldo, void *stream);

@@ -32,6 +32,7 @@ inline bool heads_ok(int q_heads, int kv_heads) {
 }
 
 constexpr int64_t kMostRows = 1LL << 30, kMostSeqs = 1LL << 24, kMostBytes = 1LL << 48;
+constexpr float kMostScale = 1099511627776.f;  // 2^40: scores stay within fp32
 
 }  // namespace
 
@@ -120,7 +121,7 @@ int itq3s_cache_attention(const void* Q, int64_t ldq, int64_t T, int q_heads, co
     int rc = cache_ok(cache);
     if (rc != 0) return rc;
     if (!heads_ok(q_heads, cache->kv_heads) || T <= 0 || seqs <= 0 || seqs > kMostSeqs || T > kMostRows / (q_heads / cache->kv_heads)) return ITQ3S_ERR_SHAPE;
-    if (ld_pages <= 0 || ld_pages > kMostRows / cache->page_tokens || max_q <= 0 || max_kv <= 0 || max_kv > kMostRows || !isfinite(scale)) return ITQ3S_ERR_SHAPE;
+    if (ld_pages <= 0 || ld_pages > kMostRows / cache->page_tokens || max_q <= 0 || max_kv <= 0 || max_kv > kMostRows || !(fabsf(scale) <= kMostScale)) return ITQ3S_ERR_SHAPE;
     if ((rc = rows_ok(Q, ldq, q_heads, cache->head_dim, 2)) != 0 || (rc = rows_ok(out, ldo, q_heads, cache->head_dim, 2)) != 0) return rc;
     if (!aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(pages, 4) || (status_flags && !aligned(status_flags, 4))) return ITQ3S_ERR_ALIGN;
     if (max_q > T) max_q = T;
@@ -134,7 +135,7 @@ int itq3s_cache_attention(const void* Q, int64_t ldq, int64_t T, int q_heads, co
 int itq3s_prompt_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T, int q_heads, int kv_heads, int head_dim,
                            const int32_t* starts, int64_t seqs, int64_t max_len, int causal, float scale, void* out, int64_t ldo, void* stream) {
     if (!Q || !K || !V || !starts || !out) return ITQ3S_ERR_NULL;
-    if (!heads_ok(q_heads, kv_heads) || !head_dim_ok(head_dim) || T <= 0 || T > kMostRows / (q_heads / kv_heads) || seqs <= 0 || seqs > kMostSeqs || max_len <= 0 || !isfinite(scale))
+    if (!heads_ok(q_heads, kv_heads) || !head_dim_ok(head_dim) || T <= 0 || T > kMostRows / (q_heads / kv_heads) || seqs <= 0 || seqs > kMostSeqs || max_len <= 0 || !(fabsf(scale) <= kMostScale))
         return ITQ3S_ERR_SHAPE;
     int rc = 0;
     if ((rc = rows_ok(Q, ldq, q_heads, head_dim, 2)) != 0 || (rc = rows_ok(K, ldk, kv_heads, head_dim, 2)) != 0 || (rc = rows_ok(V, ldv, kv_heads, head_dim, 2)) != 0 ||

@@ -50,17 +50,29 @@ template <int MASK>
 __device__ __forceinline__ float row_xor(float v) { return __builtin_bit_cast(float, row_xor_i32<MASK>(__builtin_bit_cast(int, v))); }
 
 template <int D, int MASK, typename R>
-__device__ __forceinline__ void hadamard_across(R (&v)[8]) {
+__device__ __forceinline__ void hadamard_across(R (&v)[8], int lane) {
     if constexpr (MASK < D / 8) {
-        const R sign = (lane_id() & MASK) != 0 ? (R)-1 : (R)1;
+        const R sign = (lane & MASK) != 0 ? (R)-1 : (R)1;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = __builtin_elementwise_fma(sign, v[j], row_xor<MASK>(v[j]));
     }
 }
 
+// Sum and maximum over the D / 8 lanes of a row.
+template <int D, int MASK = 1>
+__device__ __forceinline__ float row_sum(float v) {
+    if constexpr (MASK < D / 8) return row_sum<D, 2 * MASK>(v + row_xor<MASK>(v));
+    else return v;
+}
+template <int D, int MASK = 1>
+__device__ __forceinline__ float row_max(float v) {
+    if constexpr (MASK < D / 8) return row_max<D, 2 * MASK>(__builtin_fmaxf(v, row_xor<MASK>(v)));
+    else return v;
+}
+
 // The transform of a row, eight neighbouring channels a lane, without the factor 1 / sqrt(D).
 template <int D, typename R>
-__device__ __forceinline__ void hadamard(R (&v)[8]) {
+__device__ __forceinline__ void hadamard(R (&v)[8], int lane = lane_id()) {
 #pragma unroll
     for (int h = 1; h < 8; h *= 2)
 #pragma unroll
@@ -70,11 +82,11 @@ __device__ __forceinline__ void hadamard(R (&v)[8]) {
                 v[j] = a + b;
                 v[j + h] = a - b;
             }
-    hadamard_across<D, 1>(v);
-    hadamard_across<D, 2>(v);
-    hadamard_across<D, 4>(v);
-    hadamard_across<D, 8>(v);
-    hadamard_across<D, 16>(v);
+    hadamard_across<D, 1>(v, lane);
+    hadamard_across<D, 2>(v, lane);
+    hadamard_across<D, 4>(v, lane);
+    hadamard_across<D, 8>(v, lane);
+    hadamard_across<D, 16>(v, lane);
 }
 
 }  // namespace itq3s

@@ -32,10 +32,12 @@ struct AttnArgs {
     _Float16* out;
     float *part, *ml;  // [splits][T * q_heads][D], [splits][T * q_heads][2]
     uint32_t* flags;
-    int64_t ldq, ldo, ld_pages, T, pool;
+    int64_t ldq, ldo, ld_pages, T;
     float scale;  // softmax scale * log2(e) / sqrt(D)
-    int q_heads, kv_heads, group, seqs, tiles, splits, split_blocks, page_shift;
+    int q_heads, kv_heads, group, seqs, tiles, splits, split_blocks, page_shift, pool, page_units;
 };
+
+typedef const __attribute__((address_space(4))) int32_t* table_t;  // read through the scalar cache, beside the vector loads
 
 // A sequence: its rows among all query rows, its tokens in the cache, and how its blocks are split.
 struct Seq {
@@ -44,12 +46,13 @@ struct Seq {
 };
 __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int s) {
     Seq q;
-    int64_t lo = a.starts[s], hi = a.starts[s + 1];
+    const table_t starts = (table_t)(uintptr_t)a.starts, lens = (table_t)(uintptr_t)a.kv_lens;
+    int64_t lo = starts[s], hi = starts[s + 1];
     lo = lo < 0 ? 0 : lo > a.T ? a.T : lo;
     hi = hi < lo ? lo : hi > a.T ? a.T : hi;
     q.first = lo;
     q.rows = (int)(hi - lo);
-    int64_t len = a.kv_lens[s];
+    int64_t len = lens[s];
     const int64_t most = a.ld_pages << (a.page_shift + 5);
     if (len > most) {
         if (a.flags != nullptr && threadIdx.x == 0) atomicOr(a.flags, kFlagBadSlot);
@@ -63,156 +66,246 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int s) {
     return q;
 }
 
+// Across the 16-lane rows of a wavefront: sums and differences, sums, maxima of lanes l and l ^ kMask (16 or 32), by the
+// instruction that swaps such rows between two registers: handed one value twice it gives every lane both rows' values.
+template <int kMask>
+__device__ __forceinline__ floatx2 both_rows(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    uint32_t even, odd;  // (scalars: a bit cast of a vector's element takes the first one)
+    if constexpr (kMask == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        even = r[0], odd = r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        even = r[0], odd = r[1];
+    }
+    return floatx2{__builtin_bit_cast(float, even), __builtin_bit_cast(float, odd)};
+}
+template <int kMask>
+__device__ __forceinline__ float butterfly(float v, int lane) {
+    const floatx2 r = both_rows<kMask>(v);
+    return __builtin_fmaf((lane & kMask) != 0 ? -1.f : 1.f, r[1], r[0]);
+}
+__device__ __forceinline__ float sum_rows(float v) {
+    floatx2 r = both_rows<16>(v);
+    r = both_rows<32>(r[0] + r[1]);
+    return r[0] + r[1];
+}
+__device__ __forceinline__ float max_rows(float v) {
+    floatx2 r = both_rows<16>(v);
+    r = both_rows<32>(__builtin_fmaxf(r[0], r[1]));
+    return __builtin_fmaxf(r[0], r[1]);
+}
+
+// A block on its way to the matrix operands.
 template <int D>
 struct Block {
     uint32_t k[2][D / 32];
-    u32x4 v[D / 64];
-    u32x4 s[2];
-    int base;  // its first token, beyond every sequence for a block that is not there
+    u32x4 v[D / 64], s[2];
 };
 
+// Where a block is, and its first token: beyond every sequence for one that is not there.
+typedef const __attribute__((address_space(1))) unsigned char* bytes_t;
+struct Place {
+    bytes_t at;
+    int base;
+};
 template <int D>
-__device__ __forceinline__ void load_block(const AttnArgs& a, const int32_t* pages, int head, int b, Block<D>& o) {
-    int page = pages[b >> a.page_shift];
-    o.base = b * kCacheBlock;
-    if ((uint32_t)page >= (uint64_t)a.pool) {
+__device__ __forceinline__ Place find_block(const AttnArgs& a, int page, int head, int b) {
+    Place p;
+    p.base = b * kCacheBlock;
+    if ((uint32_t)page >= (uint32_t)a.pool) {
         if (a.flags != nullptr && lane_id() == 0) atomicOr(a.flags, kFlagBadSlot);
         page = 0;
-        o.base = 0x7fffff00;
+        p.base = 0x7fffff00;
     }
-    const unsigned char* const at = a.data + block_offset<D>(page, head, a.kv_heads, 1 << a.page_shift, b & ((1 << a.page_shift) - 1));
-    const int lane = lane_id(), g = lane >> 4, r = lane & 15;
+    // in units of 128 bytes: a page's fit 32 bits
+    constexpr uint32_t kUnits = kBlockBytes<D> / 128;
+    const uint64_t units = (uint64_t)(uint32_t)page * (uint32_t)a.page_units + (uint32_t)(((head << a.page_shift) + (b & ((1 << a.page_shift) - 1))) * kUnits);
+    // (one place for the wavefront: kept in scalar registers, which the products of 64 bits leave)
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)units), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(units >> 32));
+    p.at = (bytes_t)(uintptr_t)a.data + ((uint64_t)high << 32 | low) * 128;
+    asm("" : "+s"(p.at));  // lanes add 32-bit offsets to it
+    p.base = __builtin_amdgcn_readfirstlane(p.base);
+    return p;
+}
+template <int D>
+__device__ __forceinline__ void load_keys(bytes_t at, uint32_t (&k)[2][D / 32], int lane) {
+    uint32_t off = (uint32_t)((lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
+    asm volatile("" : "+v"(off));  // (32 bits wide up to the load, which adds them to scalars)
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-        const unsigned char* const kp = at + (tt * 16 + r) * (D / 2) + g * (D / 8);
         if constexpr (D == 64) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
-            o.k[tt][0] = w[0], o.k[tt][1] = w[1];
+            const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(at + tt * 8 * D + off);
+            k[tt][0] = w[0], k[tt][1] = w[1];
         } else {
 #pragma unroll
             for (int i = 0; i < D / 128; ++i) {
-                const u32x4 w = reinterpret_cast<const u32x4*>(kp)[i];
+                const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(at + tt * 8 * D + 16 * i + off);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o.k[tt][4 * i + j] = w[j];
+                for (int j = 0; j < 4; ++j) k[tt][4 * i + j] = w[j];
             }
         }
-        o.s[tt] = *reinterpret_cast<const u32x4*>(at + 32 * D + 4 * (tt * 16 + 4 * g));
     }
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h) o.v[h] = *reinterpret_cast<const u32x4*>(at + 16 * D + h * 1024 + lane * 16);
 }
-
-__device__ __forceinline__ half8 join(half2v a, half2v b, half2v c, half2v d) {
-    return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// The rotated queries of a column tile: lane (column l % 16, g = l / 16) holds channels (D/4) g .. (D/4) (g + 1) - 1, scaled by
-// a power of two into fp16's best range; returns what scores have to be multiplied with.
 template <int D>
-__device__ __forceinline__ float load_queries(const _Float16* q, bool there, float scale, half8 (&f)[D / 32]) {
-    float x[D / 4];
+__device__ __forceinline__ void load_steps(bytes_t at, u32x4 (&s)[2], int lane) {
+    uint32_t off = (uint32_t)(lane >> 4) * 16;
+    asm volatile("" : "+v"(off));  // (32 bits wide up to the load, which adds them to scalars)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        half8 h = there ? reinterpret_cast<const half8*>(q)[i] : half8{};
+    for (int tt = 0; tt < 2; ++tt) s[tt] = *(const __attribute__((address_space(1))) u32x4*)(at + 32 * D + 64 * tt + off);
+}
+template <int D>
+__device__ __forceinline__ void load_values(bytes_t at, u32x4 (&v)[D / 64], int lane) {
+    uint32_t off = (uint32_t)lane * 16;
+    asm volatile("" : "+v"(off));  // (32 bits wide up to the load, which adds them to scalars)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[8 * i + j] = (float)h[j];
-    }
+    for (int h = 0; h < D / 64; ++h) v[h] = *(const __attribute__((address_space(1))) u32x4*)(at + 16 * D + h * 1024 + off);
+}
+
+__device__ __forceinline__ half8 as_halves(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(half8, u32x4{a, b, c, d}); }
+
+// Stored digits n = c + 8 of keys: in the mantissa of 1024 (nibbles 0 and 4 of a word or of the word a byte on) or of 64
+// (nibbles 1 and 5).  What is too much, 1032 sum q of the first and 72 sum q of the second, is the accumulator's start.
+// (Mask and mantissa are one instruction if one of the two constants is in a vector register.)
+struct Mantissas {
+    uint32_t low = 0x64006400u, high = 0x54005400u;
+};
+__device__ __forceinline__ half8 key_operand(uint32_t w, const Mantissas& m) {
+    return as_halves((w & 0x000f000fu) | m.low, (w & 0x00f000f0u) | m.high, ((w >> 8) & 0x000f000fu) | m.low, ((w >> 8) & 0x00f000f0u) | m.high);
+}
+// Stored digits of values, as subnormal fp16: n 2^-24, or n 2^-20 for the upper nibbles, exactly what the matrix cores take them for.
+__device__ __forceinline__ half8 value_operand_low(uint32_t u, uint32_t w) { return as_halves(u & 0x000f000fu, (u >> 8) & 0x000f000fu, w & 0x000f000fu, (w >> 8) & 0x000f000fu); }
+__device__ __forceinline__ half8 value_operand_high(uint32_t u, uint32_t w) { return as_halves(u & 0x00f000f0u, (u >> 8) & 0x00f000f0u, w & 0x00f000f0u, (w >> 8) & 0x00f000f0u); }
+
+// The rotated queries of a wavefront's rows, as the products want them: lane (column l % 16, g = l / 16) holds channels
+// (D/4) g .. (D/4) (g + 1) - 1, scaled by a power of two into fp16's best range, in kParts parts of fp16 (two leave no
+// rounding to speak of).
+template <int D, int CT>
+struct Queries {
+    half8 f[CT][D / 32];  // the first part; the second stays in LDS, where it is read once a block
+    uint32_t row[CT];     // there, in bytes
+    float start[CT];      // of the scores' accumulators
+    float unit[CT];       // what scores are multiplied with, positive
+};
+// They are turned eight channels a lane, 512 / D rows a wavefront at a time, and change lanes through LDS: a row is kParts
+// rows of fp16, start and unit, with 8 bytes more so that neighbouring rows begin in other banks.
+template <int D, int kParts>
+constexpr int kQueryPitch = kParts * 2 * D + 16;
+template <int D, int kParts>
+__device__ __forceinline__ void turn_query(const _Float16* q, bool there, float scale, unsigned char* row, int lane) {
+    const int ch = lane % (D / 8) * 8;
+    const half8 h8 = *reinterpret_cast<const half8*>(q + ch);  // (of a row that is there, whatever the lane's is)
+    float x[8];
 #pragma unroll
-    for (int h = 1; h < D / 4; h *= 2)
-#pragma unroll
-        for (int j = 0; j < D / 4; ++j)
-            if ((j & h) == 0) {
-                const float u = x[j], v = x[j + h];
-                x[j] = u + v;
-                x[j + h] = u - v;
-            }
+    for (int j = 0; j < 8; ++j) x[j] = there ? (float)h8[j] : 0.f;
+    hadamard<D>(x, lane);
     float most = 0.f;
 #pragma unroll
-    for (int m = 16; m <= 32; m *= 2) {
-        const float sign = (lane_id() & m) != 0 ? -1.f : 1.f;
-#pragma unroll
-        for (int j = 0; j < D / 4; ++j) x[j] = __builtin_fmaf(sign, x[j], xor_lane_f32(x[j], m));
-    }
-#pragma unroll
-    for (int j = 0; j < D / 4; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[j]));
-    most = __builtin_fmaxf(most, xor_lane_f32(most, 16));
-    most = __builtin_fmaxf(most, xor_lane_f32(most, 32));
+    for (int j = 0; j < 8; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[j]));
+    most = row_max<D>(most);
     const int e = __builtin_amdgcn_frexp_expf(most);  // 0 for 0, infinities and NaN
+    const float sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+    float start = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int j = 0; j < 8; ++j) x[j] = __builtin_ldexpf(x[j], -e) * sign;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[i][j] = (_Float16)__builtin_ldexpf(x[8 * i + j], -e);
-    return __builtin_ldexpf(scale, e);
+    for (int p = 0; p < kParts; ++p) {
+        half8 f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            f[j] = (_Float16)x[j];
+            x[j] -= (float)f[j];
+            start = __builtin_fmaf((j & 2) == 0 ? -1032.f : -72.f, (float)f[j], start);  // key_operand's nibbles
+        }
+        *reinterpret_cast<half8*>(row + p * 2 * D + 2 * ch) = f;
+    }
+    start = row_sum<D>(start);
+    if (ch == 0) *reinterpret_cast<floatx2*>(row + kParts * 2 * D) = floatx2{start, scale == 0.f ? 1.f : __builtin_ldexpf(__builtin_fabsf(scale), e)};
+}
+template <int D, int CT, int kParts>
+__device__ __forceinline__ void load_queries(const unsigned char* lds, uint32_t row, int ct, Queries<D, CT>& q, int g) {
+    q.row[ct] = row + (D / 2) * g;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) q.f[ct][i] = *reinterpret_cast<const half8*>(lds + row + (D / 2) * g + 16 * i);
+    q.start[ct] = *reinterpret_cast<const float*>(lds + row + kParts * 2 * D);
+    q.unit[ct] = *reinterpret_cast<const float*>(lds + row + kParts * 2 * D + 4);
 }
 
+// O^T in the units of value_operand: accumulators of even channel tiles times 2^24, of odd ones 2^20, less `eight` (of sum 8 P',
+// in the even ones' units) each.
 template <int D, int CT>
 struct State {
-    floatx4 o[D / 16][CT];
+    floatx4 o[D / 16][CT], eight[CT];
     float m[CT], l[CT];
 };
 
-template <int D, int CT>
-__device__ __forceinline__ void attend(const Block<D>& b, const half8 (&q)[CT][D / 32], const float (&qs)[CT], const int (&see)[CT], int see_all, int len, State<D, CT>& st) {
-    const int g = lane_id() >> 4;
-    float kf[2][4], vf[2][4], ve[2][4];
+template <int D, int CT, int kParts>
+__device__ __forceinline__ void scores(const uint32_t (&k)[2][D / 32], const Mantissas& mant, const unsigned char* lds, const Queries<D, CT>& q, floatx4 (&s)[2][CT]) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = b.s[tt][i];
-            kf[tt][i] = f16_bits_to_f32(w & 0xffffu);
-            vf[tt][i] = f16_bits_to_f32(w >> 16);
-            ve[tt][i] = (float)((w >> 26) & 31u);
-        }
-    const bool edge = b.base + kCacheBlock > see_all;
-    if (edge) {  // what stands behind the sequence may be anything
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool in = b.base + tt * 16 + 4 * g + i < len;
-                kf[tt][i] = in ? kf[tt][i] : 0.f;
-                vf[tt][i] = in ? vf[tt][i] : 0.f;
-            }
-    }
-    floatx4 s[2][CT];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) s[tt][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int ct = 0; ct < CT; ++ct) s[tt][ct] = floatx4{q.start[ct], q.start[ct], q.start[ct], q.start[ct]};
+    uint32_t second = 2 * D;
+    if constexpr (kParts == 2) asm volatile("" : "+v"(second));  // (read anew for every block)
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            const uint32_t w = b.k[tt][i];
-            const half8 k = join(low_pair(w), high_pair(w), low_pair(w >> 8), high_pair(w >> 8));
+            const half8 f = key_operand(k[tt][i], mant);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) s[tt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[ct][i], s[tt][ct], 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct) {
+                s[tt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q.f[ct][i], s[tt][ct], 0, 0, 0);
+                if constexpr (kParts == 2)
+                    s[tt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, *reinterpret_cast<const half8*>(lds + q.row[ct] + second + 16 * i), s[tt][ct], 0, 0, 0);
+            }
         }
-    half8 p[CT];
+}
+
+__device__ __forceinline__ _Float16 half_of(uint32_t w, bool upper) { return __builtin_bit_cast(half2v, w)[upper ? 1 : 0]; }
+
+template <int D, int CT, int kParts>
+__device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)[2], int base, const Queries<D, CT>& q, const int (&see)[CT], int see_all, int len, State<D, CT>& st,
+                                        half8 (&p)[CT], int g) {
+    const bool edge = base + kCacheBlock > see_all;
+    if (edge) {  // what stands behind the sequence may be anything
+        asm volatile("");  // (keeps a branch a branch: most blocks are whole)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) step[tt][i] = base + tt * 16 + 4 * g + i < len ? step[tt][i] : 0u;
+    }
+    // a quarter of the upper byte of an fp16 is its exponent field and two bits more
+    float ve[2][4];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ve[tt][i] = (float)(step[tt][i] >> 24);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
+        const float unit = q.unit[ct], quarter = 0.25f / unit;
         float x[2][4], top = -__builtin_inff();
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[tt][i] = s[tt][ct][i] * kf[tt][i];
-                if (edge) {
-                    const bool seen = b.base + tt * 16 + 4 * g + i < see[ct];
-                    x[tt][i] = seen ? x[tt][i] * qs[ct] : -__builtin_inff();
-                } else {
-                    x[tt][i] *= qs[ct];
-                }
-                top = __builtin_fmaxf(top, x[tt][i] + ve[tt][i]);
-            }
-        top -= (float)kExpBias;
+            for (int i = 0; i < 4; ++i) x[tt][i] = __builtin_fmaf(s[tt][ct][i], (float)half_of(step[tt][i], false), 0.f);
+        if (edge) {
+            asm volatile("");
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[tt][i] = base + tt * 16 + 4 * g + i < see[ct] ? x[tt][i] : -__builtin_inff();
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, __builtin_fmaf(ve[tt][i], quarter, x[tt][i]));
+        top = __builtin_fmaf(top, unit, -(float)kExpBias);
         if (__builtin_amdgcn_ballot_w64(top > st.m[ct] + kHeadroom) != 0) {
-            top = __builtin_fmaxf(top, xor_lane_f32(top, 16));
-            top = __builtin_fmaxf(top, xor_lane_f32(top, 32));
-            const float m = __builtin_fmaxf(st.m[ct], top), f = __builtin_amdgcn_exp2f(st.m[ct] - m);
+            const float m = __builtin_fmaxf(st.m[ct], max_rows(top)), f = __builtin_amdgcn_exp2f(st.m[ct] - m);
             st.m[ct] = m;
             st.l[ct] *= f;
+            st.eight[ct] *= f;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] *= f;
         }
@@ -220,18 +313,23 @@ __device__ __forceinline__ void attend(const Block<D>& b, const half8 (&q)[CT][D
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(x[tt][i] - st.m[ct]);
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tt][i], unit, -st.m[ct]));
                 st.l[ct] += e;
-                p[ct][4 * tt + i] = (_Float16)(e * vf[tt][i]);
+                p[ct][4 * tt + i] = (_Float16)__builtin_fmaf(e, (float)half_of(step[tt][i], true), 0.f);
             }
     }
+}
+
+template <int D, int CT>
+__device__ __forceinline__ void products(const u32x4 (&v)[D / 64], const half8 (&p)[CT], State<D, CT>& st) {
+    const half8 eight = as_halves(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) st.eight[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p[ct], st.eight[ct], 0, 0, 0);
 #pragma unroll
     for (int h = 0; h < D / 64; ++h)
 #pragma unroll
         for (int pp = 0; pp < 2; ++pp) {
-            const uint32_t w0 = b.v[h][2 * pp], w1 = b.v[h][2 * pp + 1];
-            const half8 lo = join(low_pair(w0), low_pair(w0 >> 8), low_pair(w1), low_pair(w1 >> 8));
-            const half8 hi = join(high_pair(w0), high_pair(w0 >> 8), high_pair(w1), high_pair(w1 >> 8));
+            const half8 lo = value_operand_low(v[h][2 * pp], v[h][2 * pp + 1]), hi = value_operand_high(v[h][2 * pp], v[h][2 * pp + 1]);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 st.o[4 * h + 2 * pp][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, p[ct], st.o[4 * h + 2 * pp][ct], 0, 0, 0);
@@ -242,19 +340,14 @@ __device__ __forceinline__ void attend(const Block<D>& b, const half8 (&q)[CT][D
 
 // The transform of O^T's columns: channel 16 c + 4 g + i in accumulator c, lane group g, element i.
 template <int D, int CT>
-__device__ __forceinline__ void turn_back(floatx4 (&o)[D / 16][CT], int ct) {
-    const int lane = lane_id();
+__device__ __forceinline__ void turn_back(floatx4 (&o)[D / 16][CT], int ct, int lane) {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
         floatx4 v = o[c][ct];
         v = floatx4{v[0] + v[1], v[0] - v[1], v[2] + v[3], v[2] - v[3]};
         v = floatx4{v[0] + v[2], v[1] + v[3], v[0] - v[2], v[1] - v[3]};
 #pragma unroll
-        for (int m = 16; m <= 32; m *= 2) {
-            const float sign = (lane & m) != 0 ? -1.f : 1.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(sign, v[i], xor_lane_f32(v[i], m));
-        }
+        for (int i = 0; i < 4; ++i) v[i] = butterfly<32>(butterfly<16>(v[i], lane), lane);
         o[c][ct] = v;
     }
 #pragma unroll
@@ -268,41 +361,77 @@ __device__ __forceinline__ void turn_back(floatx4 (&o)[D / 16][CT], int ct) {
             }
 }
 
-// kOwn: every wavefront has 16 CT rows of its own; else the four of a workgroup share them and take blocks in turn.
-template <int D, int CT, bool kOwn>
-__global__ void __launch_bounds__(256) cache_attention_kernel(const AttnArgs a) {
-    constexpr int kRows = 16 * CT;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), g = lane >> 4, col = lane & 15;
+// LDS: the turned queries, of every wavefront or shared; in their place afterwards what the wavefronts have of shared rows: of each
+// (channel tile, lane row) 16 columns of four channels, with a place left free behind them, then references and sums.
+template <int D, int CT, int kWaves, bool kOwn, int kParts>
+struct Lds {
+    static constexpr int kQueries = (kOwn ? kWaves : 1) * 16 * CT * kQueryPitch<D, kParts>;
+    static constexpr int kPart = D / 4 * 17 + 8;  // floatx4
+    static constexpr int kBytes = kOwn || kWaves * kPart * 16 < kQueries ? kQueries : kWaves * kPart * 16;
+};
+
+// Sums and maxima of lanes l and l ^ kMask, ... up to l ^ (kEnd / 2).
+template <int kMask>
+__device__ __forceinline__ float with_lane(float v, int which) {  // 0: sum, 1: maximum
+    float a, b;
+    if constexpr (kMask >= 16) {
+        const floatx2 r = both_rows<kMask>(v);
+        a = r[0], b = r[1];
+    } else {
+        a = v, b = row_xor<kMask>(v);
+    }
+    return which == 0 ? a + b : __builtin_fmaxf(a, b);
+}
+template <int kMask, int kEnd>
+__device__ __forceinline__ float across(float v, int which) {
+    if constexpr (kMask < kEnd) return across<2 * kMask, kEnd>(with_lane<kMask>(v, which), which);
+    else return v;
+}
+
+// kOwn: every wavefront has 16 CT rows of its own; else those of a workgroup share them and take blocks in turn.
+template <int D, int CT, int kWaves, bool kOwn, int kParts>
+__global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <= 128 ? 4 : 2) cache_attention_kernel(const AttnArgs a) {
+    constexpr int kRows = 16 * CT, kTileRows = kOwn ? kWaves * kRows : kRows;
+    typedef Lds<D, CT, kWaves, kOwn, kParts> L;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     // heads fastest: with eight heads each die keeps to one, and its cache to that head's blocks
     int id = blockIdx.x;
     const int head = id % a.kv_heads;
     id /= a.kv_heads;
-    const int seq = id % a.seqs;
-    id /= a.seqs;
-    const int split = id / a.tiles;
+    const int first_tile = id % a.tiles;  // tiles of one piece of the cache beside each other
+    id /= a.tiles;
+    const int seq = id % a.seqs, split = id / a.seqs;
     const Seq sq = find_seq(a, seq);
     if (split > 0 && split >= sq.splits) return;
-    const int32_t* const pages = a.pages + (int64_t)seq * a.ld_pages;
+    const table_t pages = (table_t)(uintptr_t)(a.pages + (int64_t)seq * a.ld_pages);
     const int total = sq.rows * a.group;
-    extern __shared__ floatx4 meet[];
-    for (int tile = id % a.tiles; tile * (kOwn ? 4 : 1) * kRows < total; tile += a.tiles) {
-        const int row0 = (kOwn ? tile * 4 + wave : tile) * kRows;
+    extern __shared__ __align__(16) unsigned char lds[];
+    floatx4* const meet = reinterpret_cast<floatx4*>(lds);
+    const uint32_t queries = kOwn ? wave * kRows * kQueryPitch<D, kParts> : 0;
+    for (int tile = first_tile; tile * kTileRows < total; tile += a.tiles) {
+        int lane = lane_id();
+        asm volatile("" : "+v"(lane));  // (nothing that hangs on it is kept from one tile to the next)
+        const int g = lane >> 4, col = lane & 15;
+        const int row0 = tile * kTileRows + (kOwn ? wave * kRows : 0);
+        constexpr int kTurned = 512 / D;  // rows at a time
+#pragma unroll 1
+        for (int r = (kOwn ? 0 : wave) * kTurned; r < kRows; r += (kOwn ? 1 : kWaves) * kTurned) {
+            const int x = r + lane / (D / 8), row = row0 + x;
+            const bool there = row < total;
+            const int i = there ? row / a.group : 0, hq = head * a.group + (there ? row % a.group : 0);
+            turn_query<D, kParts>(a.Q + (sq.first + i) * a.ldq + (int64_t)hq * D, there, a.scale, lds + queries + x * kQueryPitch<D, kParts>, lane);
+        }
+        __syncthreads();
         State<D, CT> st;
-        half8 q[CT][D / 32];
-        float qs[CT];
+        Queries<D, CT> q;
         int see[CT];
-        int64_t at[CT];  // row among T * q_heads
-        bool there[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            const int row = row0 + ct * 16 + col;
-            there[ct] = row < total;
-            const int i = there[ct] ? row / a.group : 0, hq = head * a.group + (there[ct] ? row % a.group : 0);
-            at[ct] = (sq.first + i) * a.q_heads + hq;
-            const int v = sq.len - sq.rows + i + 1;
-            see[ct] = there[ct] && v > 0 ? v : 0;
-            qs[ct] = load_queries<D>(a.Q + (sq.first + i) * a.ldq + (int64_t)hq * D + g * (D / 4), there[ct], a.scale, q[ct]);
+            const int row = row0 + ct * 16 + col, v = sq.len - sq.rows + row / a.group + 1;
+            see[ct] = row < total && v > 0 ? v : 0;
+            load_queries<D, CT, kParts>(lds, queries + (ct * 16 + col) * kQueryPitch<D, kParts>, ct, q, g);
             st.m[ct] = kNoRow, st.l[ct] = 0.f;
+            st.eight[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
@@ -315,78 +444,126 @@ __global__ void __launch_bounds__(256) cache_attention_kernel(const AttnArgs a) 
         const int need = (see_most + kCacheBlock - 1) / kCacheBlock;
         end = end < need ? end : need;
         if (!kOwn) b += wave;
-        constexpr int kStep = kOwn ? 1 : 4;
+        constexpr int kStep = kOwn ? 1 : kWaves;
+        Mantissas mant;
+        asm volatile("" : "+v"(mant.low), "+v"(mant.high));
         if (b < end) {
-            Block<D> now, next;
-            load_block<D>(a, pages, head, b, now);
+            // What a block's part of the registers is done with is loaded for the next block at once: keys ahead by a softmax and a
+            // product, values by two products' worth of other wavefronts.  The last block is loaded twice rather than branched round.
+            Block<D> r;
+            Place now = find_block<D>(a, pages[b >> a.page_shift], head, b);
+            load_keys<D>(now.at, r.k, lane);
+            load_steps<D>(now.at, r.s, lane);
+            load_values<D>(now.at, r.v, lane);
+            int ahead = b + kStep < end ? b + kStep : b;
+            int page = pages[ahead >> a.page_shift];
             for (; b < end; b += kStep) {
-                load_block<D>(a, pages, head, b + kStep < end ? b + kStep : b, next);
-                attend<D, CT>(now, q, qs, see, see_all, sq.len, st);
+                const Place next = find_block<D>(a, page, head, ahead);
+                ahead = ahead + kStep < end ? ahead + kStep : ahead;
+                page = pages[ahead >> a.page_shift];
+                floatx4 s[2][CT];
+                scores<D, CT, kParts>(r.k, mant, lds, q, s);
+                __builtin_amdgcn_sched_barrier(0);
+                load_keys<D>(next.at, r.k, lane);
+                __builtin_amdgcn_sched_barrier(0);
+                half8 p[CT];
+                weights<D, CT, kParts>(s, r.s, now.base, q, see, see_all, sq.len, st, p, g);
+                __builtin_amdgcn_sched_barrier(0);
+                load_steps<D>(next.at, r.s, lane);
+                __builtin_amdgcn_sched_barrier(0);
+                products<D, CT>(r.v, p, st);
+                __builtin_amdgcn_sched_barrier(0);
+                load_values<D>(next.at, r.v, lane);
+                __builtin_amdgcn_sched_barrier(0);
                 now = next;
             }
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            st.l[ct] += xor_lane_f32(st.l[ct], 16);
-            st.l[ct] += xor_lane_f32(st.l[ct], 32);
+            st.l[ct] = sum_rows(st.l[ct]);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) st.o[c][ct] = c % 2 == 0 ? (st.o[c][ct] - st.eight[ct]) * 16777216.f : (st.o[c][ct] - st.eight[ct] * 16.f) * 1048576.f;
         }
-        if constexpr (!kOwn) {  // the other wavefronts' sums to the first
-            floatx4* const mine = meet + (wave - 1) * (64 * (CT * D / 16 + CT));
-            if (wave > 0) {
+        if constexpr (!kOwn) {
+            // Every wavefront leaves its sums; a row's are joined by D / 8 lanes a part, kTake parts at once.
+            static_assert(CT == 1, "one column tile");
+            __syncthreads();
+            floatx4* const mine = meet + wave * L::kPart;
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
+            for (int c = 0; c < D / 16; ++c) mine[(4 * c + g) * 17 + col] = st.o[c][0];
+            floatx2* const ml = reinterpret_cast<floatx2*>(mine + D / 4 * 17);
+            if (g == 0) ml[col] = floatx2{st.m[0], st.l[0]};
+            __syncthreads();
+            constexpr int kLanes = D / 8, kGroups = 64 / kLanes, kTake = kGroups < kWaves ? kGroups : kWaves, kAtOnce = kGroups / kTake;
+            const int grp = lane / kLanes, ch = lane % kLanes * 8;
+#pragma unroll 1
+            for (int r0 = wave * kAtOnce; r0 < 16; r0 += kWaves * kAtOnce) {
+                const int r = r0 + grp / kTake, row = row0 + r;
+                if (row0 + r0 >= total) break;
+                float m[kWaves / kTake], l = 0.f, o[8] = {}, most = kNoRow;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) mine[(ct * (D / 16) + c) * 64 + lane] = st.o[c][ct];
-                    mine[(CT * D / 16 + ct) * 64 + lane] = floatx4{st.m[ct], st.l[ct], 0.f, 0.f};
+                for (int w = 0; w < kWaves / kTake; ++w) {
+                    m[w] = reinterpret_cast<const floatx2*>(meet + (grp % kTake + w * kTake) * L::kPart + D / 4 * 17)[r][0];
+                    most = __builtin_fmaxf(most, m[w]);
+                }
+                most = across<kLanes, kLanes * kTake>(most, 1);
+#pragma unroll
+                for (int w = 0; w < kWaves / kTake; ++w) {
+                    const floatx4* const part = meet + (grp % kTake + w * kTake) * L::kPart;
+                    const float f = __builtin_amdgcn_exp2f(m[w] - most);
+                    l += reinterpret_cast<const floatx2*>(part + D / 4 * 17)[r][1] * f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const floatx4 v = part[(ch / 4 + i) * 17 + r];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[4 * i + j] += v[j] * f;
+                    }
+                }
+                l = across<kLanes, kLanes * kTake>(l, 0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = across<kLanes, kLanes * kTake>(o[j], 0);
+                const bool there = row < total && grp % kTake == 0;
+                const int64_t token = sq.first + row / a.group;
+                const int hq = head * a.group + row % a.group;
+                if (sq.splits > 1) {
+                    const int64_t part = ((int64_t)split * a.T + token) * a.q_heads + hq;
+                    if (there) {
+                        if (ch == 0) *reinterpret_cast<floatx2*>(a.ml + 2 * part) = floatx2{most, l};
+                        floatx4* const to = reinterpret_cast<floatx4*>(a.part + part * D + ch);
+                        to[0] = floatx4{o[0], o[1], o[2], o[3]};
+                        to[1] = floatx4{o[4], o[5], o[6], o[7]};
+                    }
+                } else {
+                    hadamard<D>(o, lane);
+                    const float f = l == 0.f ? 0.f : (float)(1.0 / kRootD<D>) / l;
+                    half8 h;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[j] = (_Float16)(o[j] * f);
+                    if (there) *reinterpret_cast<half8*>(a.out + token * a.ldo + (int64_t)hq * D + ch) = h;
                 }
             }
             __syncthreads();
-            if (wave == 0) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    float m = st.m[ct], l[3], f[3];
-                    const floatx4* other = meet + (CT * D / 16 + ct) * 64 + lane;
-#pragma unroll
-                    for (int w = 0; w < 3; ++w) {
-                        const floatx4 v = other[w * (64 * (CT * D / 16 + CT))];
-                        f[w] = v[0], l[w] = v[1];
-                        m = __builtin_fmaxf(m, v[0]);
-                    }
-                    const float f0 = __builtin_amdgcn_exp2f(st.m[ct] - m);
-                    st.m[ct] = m;
-                    st.l[ct] *= f0;
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) st.o[c][ct] *= f0;
-#pragma unroll
-                    for (int w = 0; w < 3; ++w) {
-                        f[w] = __builtin_amdgcn_exp2f(f[w] - m);
-                        st.l[ct] += l[w] * f[w];
-#pragma unroll
-                        for (int c = 0; c < D / 16; ++c) st.o[c][ct] += meet[w * (64 * (CT * D / 16 + CT)) + (ct * (D / 16) + c) * 64 + lane] * f[w];
-                    }
-                }
-            }
-            __syncthreads();
-            if (wave != 0) continue;
+            continue;
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
+            const int row = row0 + ct * 16 + col;
+            const bool there = row < total;
+            const int64_t token = sq.first + row / a.group;
+            const int hq = head * a.group + row % a.group;
             if (sq.splits > 1) {
-                const int64_t row = (int64_t)split * a.T * a.q_heads + at[ct];
-                if (there[ct]) {
-                    if (g == 0) {
-                        a.ml[2 * row] = st.m[ct];
-                        a.ml[2 * row + 1] = st.l[ct];
-                    }
-                    floatx4* const o = reinterpret_cast<floatx4*>(a.part + row * D);
+                const int64_t part = ((int64_t)split * a.T + token) * a.q_heads + hq;
+                if (there) {
+                    if (g == 0) *reinterpret_cast<floatx2*>(a.ml + 2 * part) = floatx2{st.m[ct], st.l[ct]};
+                    floatx4* const o = reinterpret_cast<floatx4*>(a.part + part * D);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) o[4 * c + g] = st.o[c][ct];
                 }
             } else {
-                turn_back<D, CT>(st.o, ct);
+                turn_back<D, CT>(st.o, ct, lane);
                 const float f = st.l[ct] == 0.f ? 0.f : (float)(1.0 / kRootD<D>) / st.l[ct];
-                if (there[ct]) {
-                    _Float16* const o = a.out + at[ct] / a.q_heads * a.ldo + at[ct] % a.q_heads * D + 4 * g;
+                if (there) {
+                    _Float16* const o = a.out + token * a.ldo + (int64_t)hq * D + 4 * g;
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) {
                         const floatx4 v = st.o[c][ct] * f;
@@ -398,137 +575,152 @@ __global__ void __launch_bounds__(256) cache_attention_kernel(const AttnArgs a) 
     }
 }
 
-// Joins the parts of rows whose sequence was split: a workgroup a row, D / 8 lanes a part.
+// Joins the parts of rows whose sequence was split: D / 8 lanes a part, `lanes` groups of them a row (a power of two up to a
+// workgroup's), the groups of a row beside each other.
 template <int D>
-__global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a, int groups_of_row) {
     constexpr int kLanes = D / 8, kGroups = 256 / kLanes;
-    __shared__ float weight[kMaxSplits];
-    __shared__ float top[4], sum[4];
-    __shared__ __align__(16) float meet[kGroups][D];
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+    __shared__ __align__(16) float meet[kGroups][D + 4];
+    const int tid = threadIdx.x, grp = tid / kLanes, ch = tid % kLanes * 8;
+    const int mine = grp % groups_of_row, rows_at_once = kGroups / groups_of_row;
     const Seq sq = find_seq(a, (int)blockIdx.x);
     if (sq.splits <= 1) return;
-    const int64_t stride = a.T * a.q_heads;
-    for (int64_t r = blockIdx.y; r < (int64_t)sq.rows * a.q_heads; r += gridDim.y) {
-        const int64_t row = sq.first * a.q_heads + r;
-        float m = kNoRow, l = 0.f;
-        if (tid < sq.splits) {
-            m = a.ml[2 * (tid * stride + row)];
-            l = a.ml[2 * (tid * stride + row) + 1];
-        }
-        float most = m;
+    const int64_t stride = a.T * a.q_heads, all = (int64_t)sq.rows * a.q_heads;
+    for (int64_t r0 = (int64_t)blockIdx.y * rows_at_once; r0 < all; r0 += (int64_t)gridDim.y * rows_at_once) {
+        const int64_t r = r0 + grp / groups_of_row;
+        const bool there = r < all;
+        const int64_t row = sq.first * a.q_heads + (there ? r : all - 1);
+        float m = kNoRow, l = 0.f, o[8] = {};
+        // four parts at a time, all their loads before the first is used; parts that are not there weigh nothing
+        for (int s0 = mine; s0 < sq.splits; s0 += 4 * groups_of_row) {
+            floatx2 ml[4];
+            floatx4 u[4], v[4];
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) most = __builtin_fmaxf(most, xor_lane_f32(most, x));
-        if (lane == 0) top[wave] = most;
-        __syncthreads();
-        most = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), __builtin_fmaxf(top[2], top[3]));
-        const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - most);
-        weight[tid] = w;
-        float part = l == 0.f ? 0.f : w * l;
+            for (int k = 0; k < 4; ++k) {
+                const int s = s0 + k * groups_of_row < sq.splits ? s0 + k * groups_of_row : s0;
+                ml[k] = *reinterpret_cast<const floatx2*>(a.ml + 2 * (s * stride + row));
+                const floatx4* const p = reinterpret_cast<const floatx4*>(a.part + (s * stride + row) * D + ch);
+                u[k] = p[0], v[k] = p[1];
+            }
+            float n = m;
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) part += xor_lane_f32(part, x);
-        if (lane == 0) sum[wave] = part;
-        __syncthreads();
-        const float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        const int grp = tid / kLanes, ch = tid % kLanes * 8;
-        float o[8] = {};
-        for (int s = grp; s < sq.splits; s += kGroups) {
-            const float f = weight[s];
-            const floatx4* const p = reinterpret_cast<const floatx4*>(a.part + (s * stride + row) * D + ch);
-            const floatx4 u = p[0], v = p[1];
+            for (int k = 0; k < 4; ++k) n = __builtin_fmaxf(n, ml[k][0]);
+            const float f = __builtin_amdgcn_exp2f(m - n);
+            m = n;
+            l *= f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                o[j] += f == 0.f ? 0.f : u[j] * f;
-                o[4 + j] += f == 0.f ? 0.f : v[j] * f;
+            for (int j = 0; j < 8; ++j) o[j] *= f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float h = s0 + k * groups_of_row < sq.splits ? __builtin_amdgcn_exp2f(ml[k][0] - n) : 0.f;
+                l += ml[k][1] * h;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[j] += u[k][j] * h;
+                    o[4 + j] += v[k][j] * h;
+                }
             }
         }
+        if (groups_of_row > 1) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) *reinterpret_cast<floatx4*>(&meet[grp][ch + 4 * i]) = floatx4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
-        __syncthreads();
-        if (wave == 0) {
-            float v[8] = {};
-            for (int k = 0; k < kGroups; ++k)
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<floatx4*>(&meet[grp][ch + 4 * i]) = floatx4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+            if (ch == 0) *reinterpret_cast<floatx2*>(&meet[grp][D]) = floatx2{m, l};
+            __syncthreads();
+            if (mine == 0) {
+                for (int k = 1; k < groups_of_row; ++k) {
+                    const float* const part = meet[grp + k];
+                    const floatx2 ml = *reinterpret_cast<const floatx2*>(part + D);
+                    const float n = __builtin_fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - n), h = __builtin_amdgcn_exp2f(ml[0] - n);
+                    m = n;
+                    l = l * f + ml[1] * h;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += meet[k][ch + j];
-            hadamard<D>(v);
-            const float f = total == 0.f ? 0.f : (float)(1.0 / kRootD<D>) / total;
-            half8 h;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = (_Float16)(v[j] * f);
-            if (lane < kLanes) *reinterpret_cast<half8*>(a.out + row / a.q_heads * a.ldo + row % a.q_heads * D + ch) = h;
+                    for (int j = 0; j < 8; ++j) o[j] = o[j] * f + part[ch + j] * h;
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
+        hadamard<D>(o);  // (all lanes: neighbouring groups exchange nothing)
+        const float f = l == 0.f ? 0.f : (float)(1.0 / kRootD<D>) / l;
+        half8 h;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = (_Float16)(o[j] * f);
+        if (there && mine == 0) *reinterpret_cast<half8*>(a.out + row / a.q_heads * a.ldo + row % a.q_heads * D + ch) = h;
     }
 }
 
-// How a call is cut up: CT column tiles of 16 rows a wavefront, own rows or shared ones, workgroups along rows and blocks.
+// How a call is cut up: rows of a workgroup's tile, tiles, and parts of the sequences.
 struct Plan {
-    int ct;
-    bool own;
+    bool own, wide;  // rows of their own a wavefront; sixteen wavefronts
     int64_t tiles;
     int splits, split_blocks;
 };
-Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int64_t max_q, int64_t max_kv) {
+Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
     Plan p;
-    const int64_t rows = max_q * (q_heads / kv_heads);
+    const int64_t rows = max_q * (q_heads / kv_heads), units = seqs * kv_heads, cus = cu_count();
+    const int64_t blocks = (max_kv + kCacheBlock - 1) / kCacheBlock;
     p.own = rows > 128;
-    p.ct = rows <= 16 ? 1 : 2;
-    const int64_t per = 16 * p.ct * (p.own ? 4 : 1);
+    const int64_t per = p.own ? (head_dim < 256 ? 128 : 64) : 16;
     p.tiles = (rows + per - 1) / per;
-    const int64_t blocks = (max_kv + kCacheBlock - 1) / kCacheBlock, units = seqs * kv_heads * p.tiles;
-    // parts of at least four blocks (one a wavefront), and no more of them than about eight workgroups a compute unit
-    int64_t per_split = (units * blocks + 2047) / 2048;
-    per_split = per_split < 4 ? 4 : (per_split + 3) / 4 * 4;
-    if (p.own && per_split < 16) per_split = 16;
+    // Few and short sequences: sixteen wavefronts share one, and no second launch joins parts.
+    p.wide = !p.own && head_dim <= 128 && blocks <= 64 && units * p.tiles <= cus;
+    // Else as many parts as fill the units once: four workgroups of four wavefronts each, two of those with rows of their own.
+    const int64_t places = (p.own ? 2 : 4) * cus, work = units * p.tiles * blocks;
+    int64_t per_split = p.wide ? blocks : (work + places - 1) / places;
+    const int64_t few = p.own ? 16 : 4;
+    if (per_split < few) per_split = few;
     const int64_t least = (blocks + kMaxSplits - 1) / kMaxSplits;
     if (per_split < least) per_split = least;
-    p.split_blocks = (int)per_split;
-    p.splits = (int)((blocks + per_split - 1) / per_split);
-    if (p.splits < 1) p.splits = 1;
+    p.split_blocks = (int)(per_split < blocks ? per_split : blocks);
+    p.splits = (int)((blocks + p.split_blocks - 1) / p.split_blocks);
     return p;
 }
 
-template <int D, int CT, bool kOwn>
+template <int D, int CT, int kWaves, bool kOwn, int kParts>
 int start(const AttnArgs& a, int64_t grid, hipStream_t st) {
-    constexpr int kLds = kOwn ? 0 : 3 * 64 * (CT * D / 16 + CT) * 16;
+    constexpr int kLds = Lds<D, CT, kWaves, kOwn, kParts>::kBytes;
+    static_assert(kLds <= 160 * 1024, "LDS");
     if constexpr (kLds > 65536) {
         static DeviceOnce once;
-        if (!raise_lds_limit(once, reinterpret_cast<const void*>(&cache_attention_kernel<D, CT, kOwn>), kLds)) return -6;
+        if (!raise_lds_limit(once, reinterpret_cast<const void*>(&cache_attention_kernel<D, CT, kWaves, kOwn, kParts>), kLds)) return -6;
     }
-    cache_attention_kernel<D, CT, kOwn><<<dim3((unsigned)grid), dim3(256), kLds, st>>>(a);
+    cache_attention_kernel<D, CT, kWaves, kOwn, kParts><<<dim3((unsigned)grid), dim3(64 * kWaves), kLds, st>>>(a);
     return hipGetLastError() == hipSuccess ? 0 : -6;
 }
 
 template <int D>
 int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStream_t st) {
     int rc;
-    if (p.own) rc = start<D, 2, true>(a, grid, st);
-    else if (p.ct == 1) rc = start<D, 1, false>(a, grid, st);
-    else rc = start<D, 2, false>(a, grid, st);
+    if (p.own) rc = start<D, D == 256 ? 1 : 2, 4, true, 1>(a, grid, st);
+    else if (p.wide) rc = start<D, 1, D <= 128 ? 16 : 4, false, 1>(a, grid, st);
+    else rc = start<D, 1, 4, false, 2>(a, grid, st);
     if (rc != 0 || p.splits <= 1) return rc;
-    const int64_t rows = max_q * a.q_heads;
-    combine_kernel<D><<<dim3((unsigned)a.seqs, (unsigned)(rows < 65535 ? rows : 65535)), dim3(256), 0, st>>>(a);
+    int groups = 1;
+    while (2 * groups <= p.splits && groups < 2048 / D) groups *= 2;
+    const int64_t at_once = 2048 / D / groups, rows = (max_q * a.q_heads + at_once - 1) / at_once;
+    combine_kernel<D><<<dim3((unsigned)a.seqs, (unsigned)(rows < 65535 ? rows : 65535)), dim3(256), 0, st>>>(a, groups);
     return hipGetLastError() == hipSuccess ? 0 : -6;
 }
 
 }  // namespace
 
 size_t cache_attention_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
-    const Plan p = plan_of(seqs, q_heads, kv_heads, max_q, max_kv);
+    const Plan p = plan_of(seqs, q_heads, kv_heads, head_dim, max_q, max_kv);
     if (p.splits <= 1) return 256;
     return (size_t)p.splits * (size_t)T * (size_t)q_heads * (size_t)(head_dim + 2) * 4 + 256;
 }
 
 int launch_cache_attention(const CacheAttentionCall& c, hipStream_t st) {
     const int G = c.q_heads / c.cache.kv_heads, D = c.cache.head_dim;
-    const Plan p = plan_of(c.seqs, c.q_heads, c.cache.kv_heads, c.max_q, c.max_kv);
+    const Plan p = plan_of(c.seqs, c.q_heads, c.cache.kv_heads, D, c.max_q, c.max_kv);
     AttnArgs a{};
     a.Q = c.Q, a.starts = c.starts, a.kv_lens = c.kv_lens, a.pages = c.pages, a.data = c.cache.data, a.out = c.out, a.flags = c.flags;
     a.part = static_cast<float*>(c.workspace);
     a.ml = a.part + (size_t)p.splits * (size_t)c.T * (size_t)c.q_heads * (size_t)D;
-    a.ldq = c.ldq, a.ldo = c.ldo, a.ld_pages = c.ld_pages, a.T = c.T, a.pool = c.cache.pages;
+    a.ldq = c.ldq, a.ldo = c.ldo, a.ld_pages = c.ld_pages, a.T = c.T, a.pool = (int)c.cache.pages;
     a.scale = (float)((double)c.scale * 1.44269504088896340736 / (D == 64 ? 8.0 : D == 128 ? 11.313708498984760390 : 16.0));
+    if (__builtin_fabsf(a.scale) < 1e-30f) a.scale = 0.f;  // no score leaves 2^-40 then: all weights alike
     a.q_heads = c.q_heads, a.kv_heads = c.cache.kv_heads, a.group = G, a.seqs = (int)c.seqs, a.tiles = (int)p.tiles, a.splits = p.splits, a.split_blocks = p.split_blocks;
+    a.page_units = c.cache.kv_heads * c.cache.page_blocks * (32 * D + 128) / 128;
     a.page_shift = __builtin_ctz((unsigned)c.cache.page_blocks);
     const int64_t grid = c.seqs * c.cache.kv_heads * p.tiles * p.splits;
     if (grid > 0x7fffffffLL) return -2;
