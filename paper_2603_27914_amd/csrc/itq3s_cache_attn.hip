@@ -32,33 +32,32 @@ struct AttnArgs {
     _Float16* out;
     float *part, *ml;  // [splits][T * q_heads][D], [splits][T * q_heads][2]
     uint32_t* flags;
-    int64_t ldq, ldo, ld_pages, T;
+    int64_t ldq, ldo;
     float scale;  // softmax scale * log2(e) / sqrt(D)
-    int q_heads, kv_heads, group, seqs, tiles, splits, split_blocks, page_shift, pool, page_units;
+    int q_heads, kv_heads, group, seqs, tiles, splits, split_blocks, page_shift, pool, page_units, T, ld_pages;
 };
 
 typedef const __attribute__((address_space(4))) int32_t* table_t;  // read through the scalar cache, beside the vector loads
 
 // A sequence: its rows among all query rows, its tokens in the cache, and how its blocks are split.
 struct Seq {
-    int64_t first;
-    int rows, len, blocks, per_split, splits;
+    int first, rows, len, blocks, per_split, splits;
 };
 __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int s) {
     Seq q;
     const table_t starts = (table_t)(uintptr_t)a.starts, lens = (table_t)(uintptr_t)a.kv_lens;
-    int64_t lo = starts[s], hi = starts[s + 1];
+    int lo = starts[s], hi = starts[s + 1];
     lo = lo < 0 ? 0 : lo > a.T ? a.T : lo;
     hi = hi < lo ? lo : hi > a.T ? a.T : hi;
     q.first = lo;
-    q.rows = (int)(hi - lo);
-    int64_t len = lens[s];
-    const int64_t most = a.ld_pages << (a.page_shift + 5);
+    q.rows = hi - lo;
+    int len = lens[s];
+    const int most = a.ld_pages << (a.page_shift + 5);  // at most 2^30
     if (len > most) {
         if (a.flags != nullptr && threadIdx.x == 0) atomicOr(a.flags, kFlagBadSlot);
         len = most;
     }
-    q.len = len < 0 ? 0 : (int)len;
+    q.len = len < 0 ? 0 : len;
     q.blocks = (q.len + kCacheBlock - 1) / kCacheBlock;
     const int need = (q.blocks + a.splits - 1) / a.splits;
     q.per_split = need > a.split_blocks ? need : a.split_blocks;
@@ -193,9 +192,8 @@ struct Queries {
 template <int D, int kParts>
 constexpr int kQueryPitch = kParts * 2 * D + 16;
 template <int D, int kParts>
-__device__ __forceinline__ void turn_query(const _Float16* q, bool there, float scale, unsigned char* row, int lane) {
+__device__ __forceinline__ void turn_query(half8 h8, bool there, float scale, unsigned char* row, int lane) {
     const int ch = lane % (D / 8) * 8;
-    const half8 h8 = *reinterpret_cast<const half8*>(q + ch);  // (of a row that is there, whatever the lane's is)
     float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = there ? (float)h8[j] : 0.f;
@@ -361,13 +359,21 @@ __device__ __forceinline__ void turn_back(floatx4 (&o)[D / 16][CT], int ct, int 
             }
 }
 
+// How the wavefronts of a workgroup share its rows and blocks.
+enum class Share {
+    blocks,  // 16 rows, all take blocks in turn
+    tiles,   // 16, 32 or 64 rows, as many as the sequence has: wavefronts of different rows take the same blocks at one time
+    none     // 16 CT rows of its own a wavefront, every block
+};
+
 // LDS: the turned queries, of every wavefront or shared; in their place afterwards what the wavefronts have of shared rows: of each
 // (channel tile, lane row) 16 columns of four channels, with a place left free behind them, then references and sums.
-template <int D, int CT, int kWaves, bool kOwn, int kParts>
+template <int D, int CT, int kWaves, Share kShare, int kParts>
 struct Lds {
-    static constexpr int kQueries = (kOwn ? kWaves : 1) * 16 * CT * kQueryPitch<D, kParts>;
+    static constexpr int kQueryRows = (kShare == Share::none ? kWaves : kShare == Share::tiles ? 4 : 1) * 16 * CT;
+    static constexpr int kQueries = kQueryRows * kQueryPitch<D, kParts>;
     static constexpr int kPart = D / 4 * 17 + 8;  // floatx4
-    static constexpr int kBytes = kOwn || kWaves * kPart * 16 < kQueries ? kQueries : kWaves * kPart * 16;
+    static constexpr int kBytes = kShare == Share::none || kWaves * kPart * 16 < kQueries ? kQueries : kWaves * kPart * 16;
 };
 
 // Sums and maxima of lanes l and l ^ kMask, ... up to l ^ (kEnd / 2).
@@ -388,11 +394,10 @@ __device__ __forceinline__ float across(float v, int which) {
     else return v;
 }
 
-// kOwn: every wavefront has 16 CT rows of its own; else those of a workgroup share them and take blocks in turn.
-template <int D, int CT, int kWaves, bool kOwn, int kParts>
-__global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <= 128 ? 4 : 2) cache_attention_kernel(const AttnArgs a) {
-    constexpr int kRows = 16 * CT, kTileRows = kOwn ? kWaves * kRows : kRows;
-    typedef Lds<D, CT, kWaves, kOwn, kParts> L;
+template <int D, int CT, int kWaves, Share kShare, int kParts>
+__global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cache_attention_kernel(const AttnArgs a) {
+    constexpr bool kOwn = kShare == Share::none;
+    typedef Lds<D, CT, kWaves, kShare, kParts> L;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     // heads fastest: with eight heads each die keeps to one, and its cache to that head's blocks
     int id = blockIdx.x;
@@ -401,25 +406,61 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
     const int first_tile = id % a.tiles;  // tiles of one piece of the cache beside each other
     id /= a.tiles;
     const int seq = id % a.seqs, split = id / a.seqs;
+    // The way to the first block is a chain of loads, each some hundred nanoseconds: the page of the block that this will most likely
+    // be is read beside the sequence's lengths, and the block is on its way before the queries are turned.
+    const table_t pages = (table_t)(uintptr_t)(a.pages + (int64_t)seq * a.ld_pages);
+    const int likely = (split * a.split_blocks + (kOwn ? 0 : wave)) >> a.page_shift, likely_at = likely < a.ld_pages ? likely : a.ld_pages - 1;
+    const int likely_page = pages[likely_at];
     const Seq sq = find_seq(a, seq);
     if (split > 0 && split >= sq.splits) return;
-    const table_t pages = (table_t)(uintptr_t)(a.pages + (int64_t)seq * a.ld_pages);
     const int total = sq.rows * a.group;
+    // rows of a workgroup's tile, 16 (or a wavefront's own ones) times a power of two
+    const int share = kShare != Share::tiles ? 0 : total > 32 ? 2 : total > 16 ? 1 : 0;
+    const int tile_rows = kOwn ? kWaves * 16 * CT : 16 << share;
+    const int first_row = kOwn ? wave * 16 * CT : (wave & ((1 << share) - 1)) * 16;  // of the wavefront within it
+    const int take = kOwn ? 0 : wave >> share, step = kOwn ? 1 : kWaves >> share;    // which blocks
     extern __shared__ __align__(16) unsigned char lds[];
     floatx4* const meet = reinterpret_cast<floatx4*>(lds);
-    const uint32_t queries = kOwn ? wave * kRows * kQueryPitch<D, kParts> : 0;
-    for (int tile = first_tile; tile * kTileRows < total; tile += a.tiles) {
+    for (int tile = first_tile; tile * tile_rows < total; tile += a.tiles) {
         int lane = lane_id();
         asm volatile("" : "+v"(lane));  // (nothing that hangs on it is kept from one tile to the next)
         const int g = lane >> 4, col = lane & 15;
-        const int row0 = tile * kTileRows + (kOwn ? wave * kRows : 0);
+        const int tile_row0 = tile * tile_rows, row0 = tile_row0 + first_row;
+        // rows of the wavefront see between see_all and see_most places
+        const int last = row0 + 16 * CT < total ? row0 + 16 * CT - 1 : total - 1;
+        const int see_all = sq.len - sq.rows + (row0 < total ? row0 / a.group : 0) + 1;
+        int see_most = row0 < total ? sq.len - sq.rows + last / a.group + 1 : 0;
+        see_most = see_most < 0 ? 0 : see_most;
+        int b = split * sq.per_split + take, end = split * sq.per_split + sq.per_split;
+        const int need = (see_most + kCacheBlock - 1) / kCacheBlock;
+        end = end < need ? end : need;
+        int page = likely_page;
+        if (b >= end) page = 0;
+        else if ((b >> a.page_shift) != likely_at) page = pages[b >> a.page_shift];
+
         constexpr int kTurned = 512 / D;  // rows at a time
-#pragma unroll 1
-        for (int r = (kOwn ? 0 : wave) * kTurned; r < kRows; r += (kOwn ? 1 : kWaves) * kTurned) {
-            const int x = r + lane / (D / 8), row = row0 + x;
-            const bool there = row < total;
+        // rows of the tile (of the wavefront) from r on, in the lanes' order: the row, whether it is there, its values
+        auto query_row = [&](int r, bool& there) {
+            const int row = (kOwn ? row0 : tile_row0) + r + lane / (D / 8);
+            there = row < total;
             const int i = there ? row / a.group : 0, hq = head * a.group + (there ? row % a.group : 0);
-            turn_query<D, kParts>(a.Q + (sq.first + i) * a.ldq + (int64_t)hq * D, there, a.scale, lds + queries + x * kQueryPitch<D, kParts>, lane);
+            return *reinterpret_cast<const half8*>(a.Q + (int64_t)(sq.first + i) * a.ldq + (int64_t)hq * D + lane % (D / 8) * 8);
+        };
+        const int turn_rows = kOwn ? 16 * CT : tile_rows, turn_step = (kOwn ? 1 : kWaves) * kTurned;
+        int r_turn = (kOwn ? 0 : wave) * kTurned;
+        bool there_turn;
+        half8 h_turn = query_row(r_turn < turn_rows ? r_turn : 0, there_turn);
+        Block<D> r;
+        Place now = find_block<D>(a, page, head, b < end ? b : 0);
+        load_keys<D>(now.at, r.k, lane);
+        load_steps<D>(now.at, r.s, lane);
+        load_values<D>(now.at, r.v, lane);
+        const uint32_t queries = kOwn ? wave * (16 * CT) * kQueryPitch<D, kParts> : 0;
+#pragma unroll 1
+        while (r_turn < turn_rows) {
+            turn_query<D, kParts>(h_turn, there_turn, a.scale, lds + queries + (r_turn + lane / (D / 8)) * kQueryPitch<D, kParts>, lane);
+            r_turn += turn_step;
+            if (r_turn < turn_rows) h_turn = query_row(r_turn, there_turn);
         }
         __syncthreads();
         State<D, CT> st;
@@ -429,37 +470,22 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
         for (int ct = 0; ct < CT; ++ct) {
             const int row = row0 + ct * 16 + col, v = sq.len - sq.rows + row / a.group + 1;
             see[ct] = row < total && v > 0 ? v : 0;
-            load_queries<D, CT, kParts>(lds, queries + (ct * 16 + col) * kQueryPitch<D, kParts>, ct, q, g);
+            load_queries<D, CT, kParts>(lds, queries + ((kOwn ? 0 : first_row) + ct * 16 + col) * kQueryPitch<D, kParts>, ct, q, g);
             st.m[ct] = kNoRow, st.l[ct] = 0.f;
             st.eight[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
-        // rows of the tile see between see_all and see_most places
-        const int last = row0 + kRows < total ? row0 + kRows - 1 : total - 1;
-        const int see_all = sq.len - sq.rows + (row0 < total ? row0 / a.group : 0) + 1;
-        int see_most = row0 < total ? sq.len - sq.rows + last / a.group + 1 : 0;
-        see_most = see_most < 0 ? 0 : see_most;
-        int b = split * sq.per_split, end = b + sq.per_split;
-        const int need = (see_most + kCacheBlock - 1) / kCacheBlock;
-        end = end < need ? end : need;
-        if (!kOwn) b += wave;
-        constexpr int kStep = kOwn ? 1 : kWaves;
         Mantissas mant;
         asm volatile("" : "+v"(mant.low), "+v"(mant.high));
         if (b < end) {
             // What a block's part of the registers is done with is loaded for the next block at once: keys ahead by a softmax and a
             // product, values by two products' worth of other wavefronts.  The last block is loaded twice rather than branched round.
-            Block<D> r;
-            Place now = find_block<D>(a, pages[b >> a.page_shift], head, b);
-            load_keys<D>(now.at, r.k, lane);
-            load_steps<D>(now.at, r.s, lane);
-            load_values<D>(now.at, r.v, lane);
-            int ahead = b + kStep < end ? b + kStep : b;
-            int page = pages[ahead >> a.page_shift];
-            for (; b < end; b += kStep) {
+            int ahead = b + step < end ? b + step : b;
+            page = pages[ahead >> a.page_shift];
+            for (; b < end; b += step) {
                 const Place next = find_block<D>(a, page, head, ahead);
-                ahead = ahead + kStep < end ? ahead + kStep : ahead;
+                ahead = ahead + step < end ? ahead + step : ahead;
                 page = pages[ahead >> a.page_shift];
                 floatx4 s[2][CT];
                 scores<D, CT, kParts>(r.k, mant, lds, q, s);
@@ -478,6 +504,10 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
                 now = next;
             }
         }
+        // where the results go is read again from the arguments: it would stay in scalar registers all the way
+        typedef const __attribute__((address_space(4))) AttnArgs* args_t;
+        args_t late = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(late));
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             st.l[ct] = sum_rows(st.l[ct]);
@@ -485,51 +515,49 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] = c % 2 == 0 ? (st.o[c][ct] - st.eight[ct]) * 16777216.f : (st.o[c][ct] - st.eight[ct] * 16.f) * 1048576.f;
         }
         if constexpr (!kOwn) {
-            // Every wavefront leaves its sums; a row's are joined by D / 8 lanes a part, kTake parts at once.
+            // Every wavefront leaves its sums.  A row is joined by a wavefront, D / 8 lanes a part.
             static_assert(CT == 1, "one column tile");
             __syncthreads();
             floatx4* const mine = meet + wave * L::kPart;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) mine[(4 * c + g) * 17 + col] = st.o[c][0];
-            floatx2* const ml = reinterpret_cast<floatx2*>(mine + D / 4 * 17);
-            if (g == 0) ml[col] = floatx2{st.m[0], st.l[0]};
+            if (g == 0) reinterpret_cast<floatx2*>(mine + D / 4 * 17)[col] = floatx2{st.m[0], st.l[0]};
             __syncthreads();
-            constexpr int kLanes = D / 8, kGroups = 64 / kLanes, kTake = kGroups < kWaves ? kGroups : kWaves, kAtOnce = kGroups / kTake;
+            constexpr int kLanes = D / 8, kGroups = 64 / kLanes;
             const int grp = lane / kLanes, ch = lane % kLanes * 8;
 #pragma unroll 1
-            for (int r0 = wave * kAtOnce; r0 < 16; r0 += kWaves * kAtOnce) {
-                const int r = r0 + grp / kTake, row = row0 + r;
-                if (row0 + r0 >= total) break;
-                float m[kWaves / kTake], l = 0.f, o[8] = {}, most = kNoRow;
-#pragma unroll
-                for (int w = 0; w < kWaves / kTake; ++w) {
-                    m[w] = reinterpret_cast<const floatx2*>(meet + (grp % kTake + w * kTake) * L::kPart + D / 4 * 17)[r][0];
-                    most = __builtin_fmaxf(most, m[w]);
-                }
-                most = across<kLanes, kLanes * kTake>(most, 1);
-#pragma unroll
-                for (int w = 0; w < kWaves / kTake; ++w) {
-                    const floatx4* const part = meet + (grp % kTake + w * kTake) * L::kPart;
-                    const float f = __builtin_amdgcn_exp2f(m[w] - most);
-                    l += reinterpret_cast<const floatx2*>(part + D / 4 * 17)[r][1] * f;
+            for (int r0 = wave; r0 < tile_rows; r0 += kWaves) {
+                const int row = tile_row0 + r0, r = r0 & 15;
+                if (row >= total) break;
+                float l = 0.f, o[8] = {}, most = kNoRow;
+#pragma unroll 1
+                for (int w = (r0 >> 4) + (grp << share); w < kWaves; w += kGroups << share) {
+                    const floatx4* const part = meet + w * L::kPart;
+                    const floatx2 ml = reinterpret_cast<const floatx2*>(part + D / 4 * 17)[r];
+                    const float n = __builtin_fmaxf(most, ml[0]), f = __builtin_amdgcn_exp2f(most - n), h = __builtin_amdgcn_exp2f(ml[0] - n);
+                    most = n;
+                    l = l * f + ml[1] * h;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const floatx4 v = part[(ch / 4 + i) * 17 + r];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) o[4 * i + j] += v[j] * f;
+                        for (int j = 0; j < 4; ++j) o[4 * i + j] = o[4 * i + j] * f + v[j] * h;
                     }
                 }
-                l = across<kLanes, kLanes * kTake>(l, 0);
+                const float own = most;
+                most = across<kLanes, 64>(most, 1);
+                const float f = __builtin_amdgcn_exp2f(own - most);
+                l = across<kLanes, 64>(l * f, 0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = across<kLanes, kLanes * kTake>(o[j], 0);
-                const bool there = row < total && grp % kTake == 0;
-                const int64_t token = sq.first + row / a.group;
-                const int hq = head * a.group + row % a.group;
+                for (int j = 0; j < 8; ++j) o[j] = across<kLanes, 64>(o[j] * f, 0);
+                const bool there = grp == 0;
+                const int64_t token = sq.first + row / late->group;
+                const int hq = head * late->group + row % late->group;
                 if (sq.splits > 1) {
-                    const int64_t part = ((int64_t)split * a.T + token) * a.q_heads + hq;
+                    const int64_t part = ((int64_t)split * late->T + token) * late->q_heads + hq;
                     if (there) {
-                        if (ch == 0) *reinterpret_cast<floatx2*>(a.ml + 2 * part) = floatx2{most, l};
-                        floatx4* const to = reinterpret_cast<floatx4*>(a.part + part * D + ch);
+                        if (ch == 0) *reinterpret_cast<floatx2*>(late->ml + 2 * part) = floatx2{most, l};
+                        floatx4* const to = reinterpret_cast<floatx4*>(late->part + part * D + ch);
                         to[0] = floatx4{o[0], o[1], o[2], o[3]};
                         to[1] = floatx4{o[4], o[5], o[6], o[7]};
                     }
@@ -539,23 +567,25 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
                     half8 h;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) h[j] = (_Float16)(o[j] * f);
-                    if (there) *reinterpret_cast<half8*>(a.out + token * a.ldo + (int64_t)hq * D + ch) = h;
+                    if (there) *reinterpret_cast<half8*>(late->out + token * late->ldo + (int64_t)hq * D + ch) = h;
                 }
             }
             __syncthreads();
             continue;
+        } else {
+            __syncthreads();  // (the queries' place is written again)
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const int row = row0 + ct * 16 + col;
             const bool there = row < total;
-            const int64_t token = sq.first + row / a.group;
-            const int hq = head * a.group + row % a.group;
+            const int64_t token = sq.first + row / late->group;
+            const int hq = head * late->group + row % late->group;
             if (sq.splits > 1) {
-                const int64_t part = ((int64_t)split * a.T + token) * a.q_heads + hq;
+                const int64_t part = ((int64_t)split * late->T + token) * late->q_heads + hq;
                 if (there) {
-                    if (g == 0) *reinterpret_cast<floatx2*>(a.ml + 2 * part) = floatx2{st.m[ct], st.l[ct]};
-                    floatx4* const o = reinterpret_cast<floatx4*>(a.part + part * D);
+                    if (g == 0) *reinterpret_cast<floatx2*>(late->ml + 2 * part) = floatx2{st.m[ct], st.l[ct]};
+                    floatx4* const o = reinterpret_cast<floatx4*>(late->part + part * D);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) o[4 * c + g] = st.o[c][ct];
                 }
@@ -563,7 +593,7 @@ __global__ void __launch_bounds__(64 * kWaves, kWaves == 16 ? 4 : CT == 1 && D <
                 turn_back<D, CT>(st.o, ct, lane);
                 const float f = st.l[ct] == 0.f ? 0.f : (float)(1.0 / kRootD<D>) / st.l[ct];
                 if (there) {
-                    _Float16* const o = a.out + token * a.ldo + (int64_t)hq * D + 4 * g;
+                    _Float16* const o = late->out + token * late->ldo + (int64_t)hq * D + 4 * g;
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) {
                         const floatx4 v = st.o[c][ct] * f;
@@ -585,11 +615,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a, int grou
     const int mine = grp % groups_of_row, rows_at_once = kGroups / groups_of_row;
     const Seq sq = find_seq(a, (int)blockIdx.x);
     if (sq.splits <= 1) return;
-    const int64_t stride = a.T * a.q_heads, all = (int64_t)sq.rows * a.q_heads;
+    const int64_t stride = (int64_t)a.T * a.q_heads, all = (int64_t)sq.rows * a.q_heads;
     for (int64_t r0 = (int64_t)blockIdx.y * rows_at_once; r0 < all; r0 += (int64_t)gridDim.y * rows_at_once) {
         const int64_t r = r0 + grp / groups_of_row;
         const bool there = r < all;
-        const int64_t row = sq.first * a.q_heads + (there ? r : all - 1);
+        const int64_t row = (int64_t)sq.first * a.q_heads + (there ? r : all - 1);
         float m = kNoRow, l = 0.f, o[8] = {};
         // four parts at a time, all their loads before the first is used; parts that are not there weigh nothing
         for (int s0 = mine; s0 < sq.splits; s0 += 4 * groups_of_row) {
@@ -648,9 +678,10 @@ __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a, int grou
     }
 }
 
-// How a call is cut up: rows of a workgroup's tile, tiles, and parts of the sequences.
+// How a call is cut up.
 struct Plan {
-    bool own, wide;  // rows of their own a wavefront; sixteen wavefronts
+    Share share;
+    bool wide;  // sixteen wavefronts share the blocks
     int64_t tiles;
     int splits, split_blocks;
 };
@@ -658,15 +689,15 @@ Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_
     Plan p;
     const int64_t rows = max_q * (q_heads / kv_heads), units = seqs * kv_heads, cus = cu_count();
     const int64_t blocks = (max_kv + kCacheBlock - 1) / kCacheBlock;
-    p.own = rows > 128;
-    const int64_t per = p.own ? (head_dim < 256 ? 128 : 64) : 16;
+    p.share = rows > 128 ? Share::none : rows > 16 ? Share::tiles : Share::blocks;
+    const int64_t per = p.share == Share::none ? (head_dim < 256 ? 128 : 64) : p.share == Share::tiles ? 64 : 16;
     p.tiles = (rows + per - 1) / per;
     // Few and short sequences: sixteen wavefronts share one, and no second launch joins parts.
-    p.wide = !p.own && head_dim <= 128 && blocks <= 64 && units * p.tiles <= cus;
-    // Else as many parts as fill the units once: four workgroups of four wavefronts each, two of those with rows of their own.
-    const int64_t places = (p.own ? 2 : 4) * cus, work = units * p.tiles * blocks;
+    p.wide = p.share == Share::blocks && head_dim <= 128 && blocks <= 64 && units <= cus;
+    // Else as many parts as fill the units once: four workgroups of four wavefronts each, two of eight or of those with own rows.
+    const int64_t places = (p.share == Share::blocks ? 4 : 2) * cus, work = units * p.tiles * blocks;
     int64_t per_split = p.wide ? blocks : (work + places - 1) / places;
-    const int64_t few = p.own ? 16 : 4;
+    const int64_t few = p.share == Share::none ? 16 : 4;
     if (per_split < few) per_split = few;
     const int64_t least = (blocks + kMaxSplits - 1) / kMaxSplits;
     if (per_split < least) per_split = least;
@@ -675,24 +706,25 @@ Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_
     return p;
 }
 
-template <int D, int CT, int kWaves, bool kOwn, int kParts>
+template <int D, int CT, int kWaves, Share kShare, int kParts>
 int start(const AttnArgs& a, int64_t grid, hipStream_t st) {
-    constexpr int kLds = Lds<D, CT, kWaves, kOwn, kParts>::kBytes;
+    constexpr int kLds = Lds<D, CT, kWaves, kShare, kParts>::kBytes;
     static_assert(kLds <= 160 * 1024, "LDS");
     if constexpr (kLds > 65536) {
         static DeviceOnce once;
-        if (!raise_lds_limit(once, reinterpret_cast<const void*>(&cache_attention_kernel<D, CT, kWaves, kOwn, kParts>), kLds)) return -6;
+        if (!raise_lds_limit(once, reinterpret_cast<const void*>(&cache_attention_kernel<D, CT, kWaves, kShare, kParts>), kLds)) return -6;
     }
-    cache_attention_kernel<D, CT, kWaves, kOwn, kParts><<<dim3((unsigned)grid), dim3(64 * kWaves), kLds, st>>>(a);
+    cache_attention_kernel<D, CT, kWaves, kShare, kParts><<<dim3((unsigned)grid), dim3(64 * kWaves), kLds, st>>>(a);
     return hipGetLastError() == hipSuccess ? 0 : -6;
 }
 
 template <int D>
 int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStream_t st) {
     int rc;
-    if (p.own) rc = start<D, D == 256 ? 1 : 2, 4, true, 1>(a, grid, st);
-    else if (p.wide) rc = start<D, 1, D <= 128 ? 16 : 4, false, 1>(a, grid, st);
-    else rc = start<D, 1, 4, false, 2>(a, grid, st);
+    if (p.share == Share::none) rc = start<D, D == 256 ? 1 : 2, 4, Share::none, 1>(a, grid, st);
+    else if (p.share == Share::tiles) rc = start<D, 1, 8, Share::tiles, 2>(a, grid, st);
+    else if (p.wide) rc = start<D, 1, D <= 128 ? 16 : 4, Share::blocks, D <= 128 ? 1 : 2>(a, grid, st);
+    else rc = start<D, 1, 4, Share::blocks, 2>(a, grid, st);
     if (rc != 0 || p.splits <= 1) return rc;
     int groups = 1;
     while (2 * groups <= p.splits && groups < 2048 / D) groups *= 2;
@@ -716,7 +748,7 @@ int launch_cache_attention(const CacheAttentionCall& c, hipStream_t st) {
     a.Q = c.Q, a.starts = c.starts, a.kv_lens = c.kv_lens, a.pages = c.pages, a.data = c.cache.data, a.out = c.out, a.flags = c.flags;
     a.part = static_cast<float*>(c.workspace);
     a.ml = a.part + (size_t)p.splits * (size_t)c.T * (size_t)c.q_heads * (size_t)D;
-    a.ldq = c.ldq, a.ldo = c.ldo, a.ld_pages = c.ld_pages, a.T = c.T, a.pool = (int)c.cache.pages;
+    a.ldq = c.ldq, a.ldo = c.ldo, a.ld_pages = (int)c.ld_pages, a.T = (int)c.T, a.pool = (int)c.cache.pages;
     a.scale = (float)((double)c.scale * 1.44269504088896340736 / (D == 64 ? 8.0 : D == 128 ? 11.313708498984760390 : 16.0));
     if (__builtin_fabsf(a.scale) < 1e-30f) a.scale = 0.f;  // no score leaves 2^-40 then: all weights alike
     a.q_heads = c.q_heads, a.kv_heads = c.cache.kv_heads, a.group = G, a.seqs = (int)c.seqs, a.tiles = (int)p.tiles, a.splits = p.splits, a.split_blocks = p.split_blocks;
