@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 import collections
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -106,7 +107,7 @@ def lib():
         L.itq3s_matmul_weight_side_timed.argtypes = L.itq3s_matmul_weight_side.argtypes + [ctypes.POINTER(ctypes.c_float)]
         L.itq3s_read_probe.restype = ci
         L.itq3s_read_probe.argtypes = [vp, sz, vp, vp]
-        fl, dp, cache = ctypes.c_float, ctypes.c_double, ctypes.POINTER(CacheDesc)
+        fl, dp, cache = ctypes.c_float, ctypes.c_double, vp  # (struct itq3s_cache, packed bytes)
         L.itq3s_cache_bytes.restype = sz
         L.itq3s_cache_bytes.argtypes = [i64, ci, ci, ci]
         L.itq3s_rope_frequencies.restype = ci
@@ -476,10 +477,8 @@ def itq3s_matmul_sub(codes, scales, subscales, N, K, X, dtype=torch.float32, out
 # ---- the attention half of a layer: norm and rotation, the 4-bit cache, attention
 
 
-class CacheDesc(ctypes.Structure):
-    """struct itq3s_cache"""
-
-    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+# (Decode steps make these calls for every layer, so here too the time a small call takes is the time spent on its arguments: each
+# check is one attribute or comparison, and nothing is formatted or searched for unless it fails.)
 
 
 class Cache(collections.namedtuple("Cache", "data page_tokens kv_heads head_dim")):
@@ -491,6 +490,9 @@ class Cache(collections.namedtuple("Cache", "data page_tokens kv_heads head_dim"
     def pages(self):
         one = itq3s_cache_bytes(1, self.page_tokens, self.kv_heads, self.head_dim)
         return self.data.numel() // one if one else 0
+
+
+_desc = struct.Struct("@Pqiiixxxx").pack  # struct itq3s_cache
 
 
 def itq3s_cache_bytes(pages, page_tokens, kv_heads, head_dim):
@@ -505,50 +507,51 @@ def alloc_cache(pages, page_tokens, kv_heads, head_dim, device="cuda"):
     return Cache(torch.zeros(nbytes, dtype=torch.uint8, device=device), page_tokens, kv_heads, head_dim)
 
 
+_U8, _I32, _I64, _F16T, _F32T, _F64T = torch.uint8, torch.int32, torch.int64, torch.float16, torch.float32, torch.float64
+
+
 def _need_cache(cache):
-    """-> the descriptor of a cache, checked against its tensor."""
+    """-> the descriptor of a cache, checked against its tensor (the library checks the layout)."""
     data, page_tokens, kv_heads, head_dim = cache
-    if data.dtype != torch.uint8 or not data.is_contiguous():
+    if data.dtype != _U8 or not data.is_contiguous():
         raise Itq3sError("the cache's data must be a contiguous uint8 tensor")
-    one = itq3s_cache_bytes(1, page_tokens, kv_heads, head_dim)
-    if one == 0:
+    one = kv_heads * (page_tokens // 32) * (32 * head_dim + 128)
+    if one <= 0 or page_tokens % 32:
         raise Itq3sError("bad cache: page_tokens a power of two from 32 to 65536, head_dim 64, 128 or 256, kv_heads positive")
     pages, rest = divmod(data.numel(), one)
     if pages == 0 or rest:
         raise Itq3sError("the cache holds %d bytes: not whole pages of %d" % (data.numel(), one))
-    return CacheDesc(data.data_ptr(), pages, page_tokens, kv_heads, head_dim)
+    return _desc(data.data_ptr(), pages, page_tokens, kv_heads, head_dim)
 
 
 def _need_here(*tensors):
     """Device tensors, all on the current device, whose stream the call goes to."""
-    index = None
+    if _device is None:
+        raise Itq3sError("libitq3s works on device memory only")
+    index = _device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise Itq3sError("libitq3s works on device memory only; got a CPU tensor")
-        if index is None:
-            index = _device()
-        if t.get_device() != index:
-            raise Itq3sError("every tensor of a call must be on the current device")
+        if t is not None and t.get_device() != index:
+            raise Itq3sError("every tensor of a call must be on the current device" if t.is_cuda else "libitq3s works on device memory only; got a CPU tensor")
 
 
-def _need_rows(name, t, T, width, dtypes):
-    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] != T or t.shape[1] != width or t.dtype not in dtypes:
-        raise Itq3sError("%s must be %s [%d, %d] with unit column stride" % (name, "/".join(str(d)[6:] for d in dtypes), T, width))
+def _need_rows(name, t, shape, dtype):
+    """-> row stride (a single row's has no meaning to torch)"""
+    if t.shape != shape or t.dtype != dtype or t.stride(1) != 1:
+        raise Itq3sError("%s must be %s [%d, %d] with unit column stride" % (name, str(dtype)[6:], *shape))
+    return t.stride(0) if shape[0] > 1 else shape[1]
 
 
 def _need_list(name, t, n, dtype):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
         raise Itq3sError("%s must be a contiguous %s tensor of %d" % (name, str(dtype)[6:], n))
 
 
-_FLOATS, _HALF = (torch.float32, torch.float16), (torch.float16,)
+_DTYPE = {torch.float16: F16, torch.float32: F32}
 
 
-def _ld(t):
-    """Row stride; a single row's has no meaning to torch."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _need_float(name, t):
+    if t.dim() != 2 or t.dtype not in _DTYPE:
+        raise Itq3sError("%s must be float32/float16 [T, heads * head_dim] with unit column stride" % name)
 
 
 def itq3s_rope_frequencies(rot, base=10000.0, factor=1.0, trained_tokens=0, slow_turns=1.0, fast_turns=4.0):
@@ -569,83 +572,97 @@ def itq3s_cache_append(q, k, v, positions=None, freq=None, cache=None, slots=Non
     freq: float64 [rot / 2] (the first `rot` channels of a head are rotated) or None; positions: int32 [T].
     q_norm, k_norm: float32 [head_dim] or None.  q may be None; k and v may be without a cache (head_dim is needed then).
     q_out: written if given, else allocated as `dtype`; k_out: likewise without a cache, with one only written if given."""
-    _need_here(q, k, v, positions, freq, cache.data if cache is not None else None, slots, q_norm, k_norm, q_out, k_out, status_flags)
+    _need_here(q, k, v, positions, freq, cache[0] if cache is not None else None, slots, q_norm, k_norm, q_out, k_out, status_flags)
     first = q if q is not None else k
     if first is None:
         raise Itq3sError("q or k is needed")
-    if first.dim() != 2 or first.dtype not in _FLOATS:
-        raise Itq3sError("q and k must be float32/float16 [T, heads * head_dim] with unit column stride")
-    T, in_dtype = first.shape[0], (first.dtype,)
-    desc, kv_heads = None, 1
+    _need_float("q and k", first)
+    T, in_dtype = first.shape[0], first.dtype
+    desc, q_heads, kv_heads, rot = None, 0, 1, 0
+    ldq = ldk = ldv = ldqo = ldko = 0
+    qp = kp = vp = qop = kop = None
     if cache is not None:
         desc = _need_cache(cache)
         if k is None or v is None or slots is None:
             raise Itq3sError("a cache needs k, v and slots")
         head_dim, kv_heads = cache.head_dim, cache.kv_heads
-        _need_list("slots", slots, T, torch.int64)
-        _need_rows("v", v, T, kv_heads * head_dim, in_dtype)
+        _need_list("slots", slots, T, _I64)
+        ldv, vp = _need_rows("v", v, (T, kv_heads * head_dim), in_dtype), v.data_ptr()
+        slots = slots.data_ptr()
     elif v is not None:
         raise Itq3sError("v is only needed with a cache")
+    else:
+        slots = None
     if head_dim not in (64, 128, 256):
         raise Itq3sError("head_dim must be 64, 128 or 256")
-    q_heads = rot = 0
     if k is not None:
         if cache is None:
             kv_heads = max(k.shape[-1] // head_dim, 1)
-        _need_rows("k", k, T, kv_heads * head_dim, in_dtype)
+        shape = (T, kv_heads * head_dim)
+        ldk, kp = _need_rows("k", k, shape, in_dtype), k.data_ptr()
         if k_out is None and cache is None:
-            k_out = torch.empty((T, kv_heads * head_dim), dtype=q_out.dtype if q_out is not None else dtype, device=k.device)
+            k_out = torch.empty(shape, dtype=q_out.dtype if q_out is not None else dtype, device=k.device)
+        if k_out is not None:
+            _need_float("k_out", k_out)
+            ldko, kop, dtype = _need_rows("k_out", k_out, shape, k_out.dtype), k_out.data_ptr(), k_out.dtype
     elif k_out is not None:
         raise Itq3sError("k_out without k")
     if q is not None:
-        q_heads = max(q.shape[-1] // head_dim, 1)
-        _need_rows("q", q, T, q_heads * head_dim, in_dtype)
+        q_heads = max(q.shape[1] // head_dim, 1)
+        shape = (T, q_heads * head_dim)
+        ldq, qp = _need_rows("q", q, shape, in_dtype), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty((T, q_heads * head_dim), dtype=k_out.dtype if k_out is not None else dtype, device=q.device)
-        _need_rows("q_out", q_out, T, q_heads * head_dim, _FLOATS)
+            q_out = torch.empty(shape, dtype=dtype, device=q.device)
+        _need_float("q_out", q_out)
+        if k_out is None:
+            dtype = q_out.dtype
+        ldqo, qop = _need_rows("q_out", q_out, shape, dtype), q_out.data_ptr()
     elif q_out is not None:
         raise Itq3sError("q_out without q")
-    if k_out is not None:
-        _need_rows("k_out", k_out, T, kv_heads * head_dim, _FLOATS if q_out is None else (q_out.dtype,))
     if freq is not None:
         if positions is None:
             raise Itq3sError("a rotation needs positions")
-        _need_list("freq", freq, freq.numel(), torch.float64)
-        _need_list("positions", positions, T, torch.int32)
         rot = 2 * freq.numel()
-    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if w is not None:
-            _need_list(name, w, head_dim, torch.float32)
+        _need_list("freq", freq, rot // 2, _F64T)
+        _need_list("positions", positions, T, _I32)
+        freq, positions = freq.data_ptr(), positions.data_ptr()
+    else:
+        positions = None
+    if q_norm is not None:
+        _need_list("q_norm", q_norm, head_dim, _F32T)
+        q_norm = q_norm.data_ptr()
+    if k_norm is not None:
+        _need_list("k_norm", k_norm, head_dim, _F32T)
+        k_norm = k_norm.data_ptr()
     _need_flags(status_flags)
-    out = q_out if q_out is not None else k_out
-    _check(
-        lib().itq3s_cache_append(
-            _ptr(q), _ld(q) if q is not None else 0, q_heads, _ptr(k), _ld(k) if k is not None else 0, _ptr(v), _ld(v) if v is not None else 0, T,
-            F16 if first.dtype == torch.float16 else F32, kv_heads, head_dim, _ptr(q_norm), _ptr(k_norm), eps, _ptr(positions), _ptr(freq), rot, interleaved, gain,
-            _ptr(q_out), _ld(q_out) if q_out is not None else 0, _ptr(k_out), _ld(k_out) if k_out is not None else 0,
-            F32 if out is not None and out.dtype == torch.float32 else F16, desc, _ptr(slots), _ptr(status_flags), _stream(),
-        )
+    status = lib().itq3s_cache_append(
+        qp, ldq, q_heads, kp, ldk, vp, ldv, T, _DTYPE[in_dtype], kv_heads, head_dim, q_norm, k_norm, eps, positions, freq, rot, interleaved, gain,
+        qop, ldqo, kop, ldko, _DTYPE.get(dtype, F16), desc, slots, _ptr(status_flags), _stream(),
     )
+    if status:
+        _check(status)
     return q_out, k_out
 
 
 def itq3s_cache_read(cache, slots, k_out=None, v_out=None, dtype=torch.float16, status_flags=None):
     """Rows of the cache as the values that they stand for: (K, V) [T, kv_heads * head_dim], float16 or float32, of slots [T]
     (int64; negative: zeros)."""
-    _need_here(cache.data, slots, k_out, v_out, status_flags)
+    _need_here(cache[0], slots, k_out, v_out, status_flags)
     desc = _need_cache(cache)
-    if slots.dim() != 1:
-        raise Itq3sError("slots must be a contiguous int64 tensor")
-    T, width = slots.shape[0], cache.kv_heads * cache.head_dim
-    _need_list("slots", slots, T, torch.int64)
+    T = slots.numel()
+    _need_list("slots", slots, T, _I64)
+    shape = (T, cache.kv_heads * cache.head_dim)
     if k_out is None:
-        k_out = torch.empty((T, width), dtype=v_out.dtype if v_out is not None else dtype, device=slots.device)
+        k_out = torch.empty(shape, dtype=v_out.dtype if v_out is not None else dtype, device=slots.device)
     if v_out is None:
-        v_out = torch.empty((T, width), dtype=k_out.dtype, device=slots.device)
-    _need_rows("k_out", k_out, T, width, _FLOATS)
-    _need_rows("v_out", v_out, T, width, (k_out.dtype,))
+        v_out = torch.empty(shape, dtype=k_out.dtype, device=slots.device)
+    _need_float("k_out", k_out)
+    dtype = k_out.dtype
+    ldk, ldv = _need_rows("k_out", k_out, shape, dtype), _need_rows("v_out", v_out, shape, dtype)
     _need_flags(status_flags)
-    _check(lib().itq3s_cache_read(desc, _ptr(slots), T, _ptr(k_out), _ld(k_out), _ptr(v_out), _ld(v_out), F16 if k_out.dtype == torch.float16 else F32, _ptr(status_flags), _stream()))
+    status = lib().itq3s_cache_read(desc, slots.data_ptr(), T, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, _DTYPE[dtype], _ptr(status_flags), _stream())
+    if status:
+        _check(status)
     return k_out, v_out
 
 
@@ -660,38 +677,38 @@ def itq3s_cache_attention(q, cache, q_starts, kv_lens, pages, scale=None, max_q=
 
     scale: 1 / sqrt(head_dim) if not given; max_q, max_kv: the most rows and tokens of a sequence to cut the work up for (T and what the
     page table has room for if not given); workspace: uint8, allocated here if not given."""
-    _need_here(q, cache.data, q_starts, kv_lens, pages, out, workspace, status_flags)
+    _need_here(q, cache[0], q_starts, kv_lens, pages, out, workspace, status_flags)
     desc = _need_cache(cache)
     if q.dim() != 2:
         raise Itq3sError("q must be float16 [T, q_heads * head_dim] with unit column stride")
     D = cache.head_dim
     T, q_heads = q.shape[0], max(q.shape[1] // D, 1)
-    _need_rows("q", q, T, q_heads * D, _HALF)
-    if kv_lens.dim() != 1:
-        raise Itq3sError("kv_lens must be a contiguous int32 tensor")
-    seqs = kv_lens.shape[0]
-    _need_list("kv_lens", kv_lens, seqs, torch.int32)
-    _need_list("q_starts", q_starts, seqs + 1, torch.int32)
-    if pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] != seqs or pages.shape[1] < 1 or pages.stride(1) != 1 or (seqs > 1 and pages.stride(0) != pages.shape[1]):
+    shape = (T, q_heads * D)
+    ldq = _need_rows("q", q, shape, _F16T)
+    seqs = kv_lens.numel()
+    _need_list("kv_lens", kv_lens, seqs, _I32)
+    _need_list("q_starts", q_starts, seqs + 1, _I32)
+    if pages.dtype != _I32 or pages.dim() != 2 or pages.shape[0] != seqs or pages.shape[1] < 1 or not pages.is_contiguous():
         raise Itq3sError("pages must be a contiguous int32 tensor [%d, pages]" % seqs)
+    ld_pages = pages.shape[1]
     if out is None:
-        out = torch.empty((T, q_heads * D), dtype=torch.float16, device=q.device)
-    _need_rows("out", out, T, q_heads * D, _HALF)
+        out = torch.empty(shape, dtype=_F16T, device=q.device)
+    ldo = _need_rows("out", out, shape, _F16T)
     _need_flags(status_flags)
     if max_q is None:
         max_q = T
     if max_kv is None:
-        max_kv = pages.shape[1] * cache.page_tokens
+        max_kv = ld_pages * cache.page_tokens
     if workspace is None:
-        workspace = torch.empty(itq3s_cache_attention_workspace_bytes(T, seqs, q_heads, cache.kv_heads, D, max_q, max_kv), dtype=torch.uint8, device=q.device)
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        workspace = torch.empty(itq3s_cache_attention_workspace_bytes(T, seqs, q_heads, cache.kv_heads, D, max_q, max_kv), dtype=_U8, device=q.device)
+    elif workspace.dtype != _U8 or not workspace.is_contiguous():
         raise Itq3sError("workspace must be a contiguous uint8 tensor")
-    _check(
-        lib().itq3s_cache_attention(
-            _ptr(q), _ld(q), T, q_heads, desc, _ptr(q_starts), _ptr(kv_lens), seqs, _ptr(pages), pages.shape[1], max_q, max_kv, D**-0.5 if scale is None else scale,
-            _ptr(out), _ld(out), _ptr(workspace), workspace.numel(), _ptr(status_flags), _stream(),
-        )
+    status = lib().itq3s_cache_attention(
+        q.data_ptr(), ldq, T, q_heads, desc, q_starts.data_ptr(), kv_lens.data_ptr(), seqs, pages.data_ptr(), ld_pages, max_q, max_kv, D**-0.5 if scale is None else scale,
+        out.data_ptr(), ldo, workspace.data_ptr(), workspace.numel(), _ptr(status_flags), _stream(),
     )
+    if status:
+        _check(status)
     return out
 
 
@@ -706,20 +723,19 @@ def itq3s_prompt_attention(q, k, v, head_dim, starts, max_len=None, causal=True,
     if q.dim() != 2 or k.dim() != 2:
         raise Itq3sError("q and k must be float16 [T, heads * head_dim] with unit column stride")
     T, q_heads, kv_heads = q.shape[0], max(q.shape[1] // head_dim, 1), max(k.shape[1] // head_dim, 1)
-    _need_rows("q", q, T, q_heads * head_dim, _HALF)
-    _need_rows("k", k, T, kv_heads * head_dim, _HALF)
-    _need_rows("v", v, T, kv_heads * head_dim, _HALF)
-    if starts.dim() != 1 or starts.shape[0] < 2:
+    shape, kv_shape = (T, q_heads * head_dim), (T, kv_heads * head_dim)
+    ldq, ldk, ldv = _need_rows("q", q, shape, _F16T), _need_rows("k", k, kv_shape, _F16T), _need_rows("v", v, kv_shape, _F16T)
+    seqs = starts.numel() - 1
+    if seqs < 1:
         raise Itq3sError("starts must be a contiguous int32 tensor of at least two")
-    seqs = starts.shape[0] - 1
-    _need_list("starts", starts, seqs + 1, torch.int32)
+    _need_list("starts", starts, seqs + 1, _I32)
     if out is None:
-        out = torch.empty((T, q_heads * head_dim), dtype=torch.float16, device=q.device)
-    _need_rows("out", out, T, q_heads * head_dim, _HALF)
-    _check(
-        lib().itq3s_prompt_attention(
-            _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(v), _ld(v), T, q_heads, kv_heads, head_dim, _ptr(starts), seqs, T if max_len is None else max_len, causal,
-            head_dim**-0.5 if scale is None else scale, _ptr(out), _ld(out), _stream(),
-        )
+        out = torch.empty(shape, dtype=_F16T, device=q.device)
+    ldo = _need_rows("out", out, shape, _F16T)
+    status = lib().itq3s_prompt_attention(
+        q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, T, q_heads, kv_heads, head_dim, starts.data_ptr(), seqs, T if max_len is None else max_len, causal,
+        head_dim**-0.5 if scale is None else scale, out.data_ptr(), ldo, _stream(),
     )
+    if status:
+        _check(status)
     return out

@@ -78,10 +78,25 @@ def memory():
     return buf, ctypes.c_void_p(at), ctypes.c_void_p(at + 8), ctypes.c_void_p(at + 2)
 
 
+class CacheDesc(ctypes.Structure):
+    """struct itq3s_cache"""
+
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
 def desc(data, pages=1, page_tokens=32, kv_heads=2, head_dim=64):
+    return ctypes.pointer(CacheDesc(data.value if data is not None else None, pages, page_tokens, kv_heads, head_dim))
+
+
+def test_the_binding_packs_the_descriptor_as_c_does():
+    import torch
+
     from paper_2603_27914_amd import binding
 
-    return binding.CacheDesc(data.value if data is not None else None, pages, page_tokens, kv_heads, head_dim)
+    data = torch.zeros(3 * 5 * 2 * (32 * 64 + 128), dtype=torch.uint8)
+    packed = binding._need_cache(binding.Cache(data, 64, 5, 64))
+    d = CacheDesc.from_buffer_copy(packed)
+    assert len(packed) == ctypes.sizeof(CacheDesc) and (d.data, d.pages, d.page_tokens, d.kv_heads, d.head_dim) == (data.data_ptr(), 3, 64, 5, 64)
 
 
 def test_append_refuses(L, memory):
