@@ -322,7 +322,7 @@ int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, co
  *   Q, out T x (q_heads * head_dim), K, V T x (kv_heads * head_dim), all fp16;  out must not overlap the inputs
  *   starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it)
  *   max_len  the most rows of a sequence that the work is cut up for (longer ones are computed all the same, slower)
- *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  |scale| up to 2^40;  no workspace */
+ *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  ldk and ldv up to 2^23;  |scale| up to 2^40;  no workspace */
 int itq3s_prompt_attention(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int q_heads,
                            int kv_heads, int head_dim, const int32_t *starts, int64_t seqs, int64_t max_len, int causal, float scale,
                            void *out, int64_t ldo, void *stream);

@@ -31,7 +31,7 @@ inline bool heads_ok(int q_heads, int kv_heads) {
     return q_heads > 0 && q_heads <= 65536 && kv_heads > 0 && kv_heads <= 1024 && q_heads % kv_heads == 0;
 }
 
-constexpr int64_t kMostRows = 1LL << 30, kMostSeqs = 1LL << 24, kMostBytes = 1LL << 48;
+constexpr int64_t kMostRows = 1LL << 30, kMostSeqs = 1LL << 24, kMostBytes = 1LL << 48, kMostStride = 1LL << 23;
 constexpr float kMostScale = 1099511627776.f;  // 2^40: scores stay within fp32
 
 }  // namespace
@@ -141,6 +141,7 @@ int itq3s_prompt_attention(const void* Q, int64_t ldq, const void* K, int64_t ld
     if ((rc = rows_ok(Q, ldq, q_heads, head_dim, 2)) != 0 || (rc = rows_ok(K, ldk, kv_heads, head_dim, 2)) != 0 || (rc = rows_ok(V, ldv, kv_heads, head_dim, 2)) != 0 ||
         (rc = rows_ok(out, ldo, q_heads, head_dim, 2)) != 0)
         return rc;
+    if (ldk > kMostStride || ldv > kMostStride) return ITQ3S_ERR_SHAPE;
     if (!aligned(starts, 4)) return ITQ3S_ERR_ALIGN;
     const itq3s::PromptCall c{static_cast<const _Float16*>(Q), static_cast<const _Float16*>(K), static_cast<const _Float16*>(V), ldq, ldk, ldv, T, q_heads, kv_heads, head_dim,
                               starts, seqs, max_len < T ? max_len : T, causal != 0, scale, static_cast<_Float16*>(out), ldo};
