@@ -212,14 +212,31 @@ struct Pipe {
     int see[2];
 };
 
+// A lane's places in a tile, in bytes: of the key chunk of step k in its row, of the value chunk of channel tile c in its row.
 template <int D>
-__device__ __forceinline__ half8 key_part(const _Float16* ks, int t, int k, int lane) {
-    return *reinterpret_cast<const half8*>(ks + k_at<D>(32 * (t & 1) + (lane & 31), 2 * k + (lane >> 5)));
+struct Places {
+    uint32_t k[D / 16], v[D / 32];
+};
+template <int D>
+__device__ __forceinline__ Places<D> find_places(int lane) {
+    Places<D> p;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) p.k[k] = (uint32_t)k_at<D>(lane & 31, 2 * k + (lane >> 5)) * 2;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        const int r = 4 * (lane >> 5) + ((lane >> 2) & 3), ch = 32 * c + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        p.v[c] = (uint32_t)(v_at<D>(r, ch / 8) + (ch & 4)) * 2;
+    }
+    return p;
+}
+// (32 rows of a tile from `at` on; the permutation of a row's chunks repeats every 16 rows of keys, every 8 of values)
+template <int D>
+__device__ __forceinline__ half8 key_part(const unsigned char* at, const Places<D>& p, int k) {
+    return *reinterpret_cast<const half8*>(at + p.k[k]);
 }
 template <int D>
-__device__ __forceinline__ half8 value_part(const _Float16* vs, int t, int k, int c, int lane) {
-    const int r = 32 * (t & 1) + 16 * k + 4 * (lane >> 5) + ((lane >> 2) & 3), ch = 32 * c + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const half4 u = read_turned(vs + v_at<D>(r, ch / 8) + (ch & 4)), w = read_turned(vs + v_at<D>(r + 8, ch / 8) + (ch & 4));
+__device__ __forceinline__ half8 value_part(const unsigned char* at, const Places<D>& p, int k, int c) {
+    const half4 u = read_turned(reinterpret_cast<const _Float16*>(at + p.v[c] + 16 * k * D * 2)), w = read_turned(reinterpret_cast<const _Float16*>(at + p.v[c] + (16 * k + 8) * D * 2));
     return half8{u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
 }
 
@@ -249,7 +266,7 @@ __device__ __forceinline__ void set_reference(Pipe<D>& w, int t0, int all, float
 // One half step: column tile X's scores of tokens t + 1 and products of tokens t on the matrix cores, the other one's weights on the
 // vector ALU (of t for X = 0, of t + 1 for X = 1).  In the second half the operands of step t + 1 are read.
 template <int D, int X>
-__device__ __forceinline__ void half_step(Pipe<D>& w, const _Float16* kn, const _Float16* vn, int t, float scale, int lane) {
+__device__ __forceinline__ void half_step(Pipe<D>& w, const unsigned char* kn, const unsigned char* vn, const Places<D>& places, float scale) {
     constexpr int Y = 1 - X;
     floatx16 s;
 #pragma unroll
@@ -257,14 +274,14 @@ __device__ __forceinline__ void half_step(Pipe<D>& w, const _Float16* kn, const 
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.kf[k], w.q[X][k], s, 0, 0, 0);
-        if constexpr (X == 1) w.kf[k] = key_part<D>(kn, t + 2, k, lane);
+        if constexpr (X == 1) w.kf[k] = key_part<D>(kn, places, k);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
             w.o[X][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.vf[k][c], w.p[X][k], w.o[X][c], 0, 0, 0);
-            if constexpr (X == 1) w.vf[k][c] = value_part<D>(vn, t + 1, k, c, lane);
+            if constexpr (X == 1) w.vf[k][c] = value_part<D>(vn, places, k, c);
         }
     const float m = w.m[Y];
     float l = 0.f;
@@ -277,16 +294,24 @@ __device__ __forceinline__ void half_step(Pipe<D>& w, const _Float16* kn, const 
     w.l[Y] += l;
     w.s[X] = s;
     asm volatile("" : "+v"(w.p[Y][0]), "+v"(w.p[Y][1]), "+v"(w.l[Y]));  // (made here, beside the products, and not where they are used)
+    // a matrix instruction (32 cycles), then what fits beside it
+#pragma unroll
+    for (int i = 0; i < 3 * D / 32; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (X == 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, X == 1 ? 5 : 4, 0);
+    }
 }
 
 template <int D>
 __global__ void __launch_bounds__(256, 1) prompt_pipe_kernel(const PromptArgs a) {
     constexpr int kChunks = kTile<D> * D / 8 / 256, kBuffers = 3;
-    extern __shared__ __align__(1024) _Float16 tiles[];  // three of keys, three of values
-    _Float16* const ks = tiles;
-    _Float16* const vs = tiles + kBuffers * kTile<D> * D;
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)tiles;
+    constexpr int kTileBytes = kTile<D> * D * 2, kValues = kBuffers * kTileBytes;
+    extern __shared__ __align__(1024) unsigned char lds[];  // three tiles of keys, three of values
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = lane_id(), hi = lane >> 5, col = lane & 31;
+    const Places<D> places = find_places<D>(lane);
     int id = blockIdx.x;
     const int head = id % a.kv_heads;
     id /= a.kv_heads;
@@ -315,11 +340,11 @@ __global__ void __launch_bounds__(256, 1) prompt_pipe_kernel(const PromptArgs a)
             const int rows = len - t0 < kTile<D> ? len - t0 : kTile<D>;
             const u32x4 kd = rows_descriptor(kb + t0 * a.ldk, rows > 0 ? ((rows - 1) * a.ldk + D) * 2 : 0);
             const u32x4 vd = rows_descriptor(vb + t0 * a.ldv, rows > 0 ? ((rows - 1) * a.ldv + D) * 2 : 0);
-            const uint32_t to = lds_base + (uint32_t)(buffer * kTile<D> * D * 2 + wave * 1024);
+            const uint32_t to = lds_base + (uint32_t)(buffer * kTileBytes + wave * 1024);
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) {
                 copy_to_lds(kd, k_off + (int)(u * (2048 / D) * 2 * a.ldk), to + u * 4096);
-                copy_to_lds(vd, v_off + (int)(u * (2048 / D) * 2 * a.ldv), to + kBuffers * kTile<D> * D * 2 + u * 4096);
+                copy_to_lds(vd, v_off + (int)(u * (2048 / D) * 2 * a.ldv), to + kValues + u * 4096);
             }
         };
         sync_copies();  // (the tiles before are read)
@@ -348,15 +373,15 @@ __global__ void __launch_bounds__(256, 1) prompt_pipe_kernel(const PromptArgs a)
             for (int x = 0; x < 16; ++x) s[0][x] = s[1][x] = 0.f;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-                const half8 f = key_part<D>(ks, 0, k, lane);
+                const half8 f = key_part<D>(lds, places, k);
                 s[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, w.q[0][k], s[0], 0, 0, 0);
                 s[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, w.q[1][k], s[1], 0, 0, 0);
-                w.kf[k] = key_part<D>(ks, 1, k, lane);
+                w.kf[k] = key_part<D>(lds + 64 * D, places, k);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) w.vf[k][c] = value_part<D>(vs, 0, k, c, lane);
+                for (int c = 0; c < D / 32; ++c) w.vf[k][c] = value_part<D>(lds + kValues, places, k, c);
             w.s[0] = s[0], w.s[1] = s[1];
             set_reference<D, 0>(w, 0, all, a.scale, hi);
             set_reference<D, 1>(w, 0, all, a.scale, hi);
@@ -377,9 +402,9 @@ __global__ void __launch_bounds__(256, 1) prompt_pipe_kernel(const PromptArgs a)
             for (int h = 0; h < 2; ++h) {
                 const int t = 2 * r + h;
                 if (t < steps) {
-                    half_step<D, 0>(w, nullptr, nullptr, t, a.scale, lane);
+                    half_step<D, 0>(w, nullptr, nullptr, places, a.scale);
                     set_reference<D, 0>(w, 32 * t + 32, all, a.scale, hi);
-                    half_step<D, 1>(w, ks + after * kTile<D> * D, vs + (h == 0 ? buffer : after) * kTile<D> * D, t, a.scale, lane);
+                    half_step<D, 1>(w, lds + after * kTileBytes + 64 * D * h, lds + kValues + (h == 0 ? buffer * kTileBytes + 64 * D : after * kTileBytes), places, a.scale);
                     set_reference<D, 1>(w, 32 * t + 32, all, a.scale, hi);
                 }
             }
