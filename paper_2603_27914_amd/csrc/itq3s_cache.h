@@ -59,14 +59,14 @@ __device__ __forceinline__ void hadamard_across(R (&v)[8], int lane) {
 }
 
 // Sum and maximum over the D / 8 lanes of a row.
-template <int D, int MASK = 1>
-__device__ __forceinline__ float row_sum(float v) {
+template <int D, int MASK = 1, typename R>
+__device__ __forceinline__ R row_sum(R v) {
     if constexpr (MASK < D / 8) return row_sum<D, 2 * MASK>(v + row_xor<MASK>(v));
     else return v;
 }
-template <int D, int MASK = 1>
-__device__ __forceinline__ float row_max(float v) {
-    if constexpr (MASK < D / 8) return row_max<D, 2 * MASK>(__builtin_fmaxf(v, row_xor<MASK>(v)));
+template <int D, int MASK = 1, typename R>
+__device__ __forceinline__ R row_max(R v) {
+    if constexpr (MASK < D / 8) return row_max<D, 2 * MASK>(__builtin_elementwise_max(v, row_xor<MASK>(v)));
     else return v;
 }
 

@@ -47,9 +47,6 @@ __device__ __forceinline__ void store8(float* p, const R (&v)[8]) {
     for (int i = 0; i < 2; ++i) reinterpret_cast<floatx4*>(p)[i] = floatx4{(float)v[4 * i], (float)v[4 * i + 1], (float)v[4 * i + 2], (float)v[4 * i + 3]};
 }
 
-__device__ __forceinline__ float xor_lane(float v, int m) { return xor_lane_f32(v, m); }
-__device__ __forceinline__ double xor_lane(double v, int m) { return xor_lane_f64(v, m); }
-
 // sine and cosine in 64 bits: the angle less the nearest multiple of pi/2 (pi/2 in two parts, products by fused
 // multiply-add: exact to 1e-17 for the 2^31 positions there are), then the Taylor series, whose first left-out terms are
 // (pi/4)^19 / 19! = 8e-20 and (pi/4)^18 / 18! = 2e-18.
@@ -100,69 +97,75 @@ struct Rows {
     __device__ static __forceinline__ int channel() { return lane_id() % kLanes * 8; }
 };
 
-// Sines and cosines of a lane's channels (pairs of channels where they are interleaved), gain and sign of the sine in.
+// What a lane's channels and their partners are multiplied with: cosines and sines (pairs of channels have theirs in common where
+// they are interleaved) times gain and the norm's weights.
 template <typename R>
 struct Turns {
-    R c[8], s[8];
+    R own[8], other[8];
 };
 template <typename R>
-__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, int ch, Turns<R>& t) {
-    const double pos = (double)a.positions[token], gain = (double)a.gain;
+__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, int ch, bool turned, const float* norm, Turns<R>& t) {
     const int half = a.rot / 2;
     const bool upper = ch >= half;
+    const int mate = turned && !a.interleaved ? (upper ? ch - half : ch + half) : ch;
+    float w[8], wm[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = wm[j] = 1.f;
+    if (norm != nullptr) {
+        load8(norm + ch, w);
+        load8(norm + mate, wm);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.own[j] = (R)w[j], t.other[j] = (R)0;
+    if (!turned) return;
+    const double pos = (double)a.positions[token], gain = (double)a.gain;
     double c = 0.0, s = 0.0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (j % 2 == 0 || !a.interleaved) turn(pos * a.freq[a.interleaved ? (ch + j) / 2 : (upper ? ch - half : ch) + j], c, s);
         const bool second = a.interleaved ? j % 2 == 1 : upper;  // of its pair
-        t.c[j] = (R)(c * gain);
-        t.s[j] = (R)((second ? s : -s) * gain);
+        t.own[j] = (R)(c * gain * (double)w[j]);
+        t.other[j] = (R)((second ? s : -s) * gain * (double)(a.interleaved ? w[j ^ 1] : wm[j]));
     }
 }
 
-// One row through norm and rotation.
+// One row through norm and rotation.  Partners' values come as they are: the norm's factor is the row's, and waits for the end.
 template <int D, typename R, typename In>
-__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const In (&x)[8], const float (&w)[8], const float (&wp)[8], bool normed, bool turned, int partner,
-                                              const Turns<R>& t, R (&y)[8]) {
+__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const In (&x)[8], bool normed, int partner, const Turns<R>& t, R (&y)[8]) {
     R f = (R)1;
     if (normed) {
         R sum = (R)0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = sum + (R)x[j] * (R)x[j];
-#pragma unroll
-        for (int m = 1; m < Rows<D>::kLanes; m *= 2) sum = sum + xor_lane(sum, m);
+        for (int j = 0; j < 8; ++j) sum = __builtin_elementwise_fma((R)x[j], (R)x[j], sum);
+        sum = row_sum<D>(sum);
         f = (R)1 / __builtin_elementwise_sqrt(sum * (R)(1.0 / D) + (R)a.eps);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = normed ? (R)x[j] * f * (R)w[j] : (R)x[j];
-    if (a.rot == 0) return;
-    R other[8];
-    if (a.interleaved) {
+    for (int j = 0; j < 8; ++j) y[j] = (R)x[j] * t.own[j];
+    if (a.rot != 0) {
+        R other[8];
+        if (a.interleaved) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) other[j] = y[j ^ 1];
-    } else {  // the partner's eight channels are another lane's: its values as they came, the norm's factor is the row's
+            for (int j = 0; j < 8; ++j) other[j] = (R)x[j ^ 1];
+        } else if constexpr (std::is_same<In, _Float16>::value) {  // two values a word
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (std::is_same<In, _Float16>::value) {
-                // two values a word
-                if (j % 2 == 0) {
-                    const uint32_t mine = (uint32_t)__builtin_bit_cast(uint16_t, x[j]) | (uint32_t)__builtin_bit_cast(uint16_t, x[j + 1]) << 16;
-                    const uint32_t got = (uint32_t)__shfl((int)mine, partner, 64);
-                    other[j] = (R)__builtin_bit_cast(_Float16, (uint16_t)got);
-                    other[j + 1] = (R)__builtin_bit_cast(_Float16, (uint16_t)(got >> 16));
-                }
-            } else {
-                other[j] = (R)__shfl(x[j], partner, 64);
+            for (int j = 0; j < 8; j += 2) {
+                const uint32_t mine = (uint32_t)__builtin_bit_cast(uint16_t, x[j]) | (uint32_t)__builtin_bit_cast(uint16_t, x[j + 1]) << 16;
+                const uint32_t got = (uint32_t)__shfl((int)mine, partner, 64);
+                other[j] = (R)__builtin_bit_cast(_Float16, (uint16_t)got);
+                other[j + 1] = (R)__builtin_bit_cast(_Float16, (uint16_t)(got >> 16));
             }
-        }
-        if (normed) {
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) other[j] = other[j] * f * (R)wp[j];
+            for (int j = 0; j < 8; ++j) other[j] = (R)__shfl(x[j], partner, 64);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = __builtin_elementwise_fma(other[j], t.other[j], y[j]);
     }
+    if (normed) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (turned) y[j] = y[j] * t.c[j] + other[j] * t.s[j];
+        for (int j = 0; j < 8; ++j) y[j] = y[j] * f;
+    }
 }
 
 // One row into the cache: transform, step, digits.  Rows without a slot do everything but the stores.
@@ -176,11 +179,8 @@ __device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8]
         finite = finite && __builtin_fabs(v[j]) <= 1.7976931348623157e308;
         most = __builtin_fmax(most, __builtin_fabs(v[j]));
     }
-#pragma unroll
-    for (int m = 1; m < Rows<D>::kLanes; m *= 2) most = __builtin_fmax(most, xor_lane_f64(most, m));
-    int bad = finite ? 0 : 1;
-#pragma unroll
-    for (int m = 1; m < Rows<D>::kLanes; m *= 2) bad |= xor_lane_i32(bad, m);
+    most = row_max<D>(finite ? most : __builtin_inf());
+    const bool bad = !(most <= 1.7976931348623157e308);
     const float s32 = (float)(most * (1.0 / (7.5 * kRootD<D>)));
     const bool sat = s32 > 65504.f;
     _Float16 s = (_Float16)(sat ? 65504.f : s32);
@@ -247,44 +247,51 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, 
         if (here && slot >= a.slots_end && ch == 0 && a.flags != nullptr) atomicOr(a.flags, kFlagBadSlot);
         if (!live) slot = 0;
     }
-    Turns<R> t;
-    float w[8], wp[8];
-    const int half = a.rot / 2, pch = ch < half ? ch + half : ch - half;
-    const bool turned = kWhat != 2 && ch < a.rot;
-    const int partner = lane_id() + (turned ? pch - ch : 0) / 8;
-    const float* const norm = kWhat == 0 ? a.q_norm : kWhat == 1 ? a.k_norm : nullptr;
-    if constexpr (kWhat != 2) {
-        if (turned) find_turns<R>(a, tok, ch, t);
-        if (norm != nullptr) {
-            load8(norm + ch, w);
-            load8(norm + (turned ? pch : ch), wp);
-        }
-    }
     const int step = by_token ? 1 : Rows<D>::kRows;
     const int heads = kWhat == 0 ? a.q_heads : a.kv_heads;
-    In x[8];
-    {
-        const int h = by_token ? h0 : h0 + row;
-        load8(src + (int64_t)(h < heads ? h : heads - 1) * D, x);
+    // kBatch rows are on their way while as many are worked on
+    constexpr int kBatch = kWhat == 0 ? 4 : 2;
+    auto head_of = [&](int hb) { return by_token ? hb : hb + row; };
+    In x[kBatch][8], next[kBatch][8];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        const int h = head_of(h0 + b * step);
+        load8(src + (int64_t)(h < heads ? h : heads - 1) * D, x[b]);
     }
-    for (int hb = h0; hb < h1; hb += step) {
-        const int h = by_token ? hb : hb + row;
-        In next[8];
-        const int hn = h + step;
-        load8(src + (int64_t)(hn < heads ? hn : heads - 1) * D, next);
-        R y[8];
-        if constexpr (kWhat == 2) {
+    const int half = a.rot / 2;
+    const bool turned = kWhat != 2 && ch < a.rot;
+    const int partner = lane_id() + (turned ? (ch < half ? half : -half) : 0) / 8;
+    const float* const norm = kWhat == 0 ? a.q_norm : kWhat == 1 ? a.k_norm : nullptr;
+    Turns<R> t;
+    if constexpr (kWhat != 2) find_turns<R>(a, tok, ch, turned, norm, t);
+    for (int hb = h0; hb < h1; hb += kBatch * step) {
+        if (hb + kBatch * step < h1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (R)x[j];
-        } else {
-            norm_and_turn<D>(a, x, w, wp, norm != nullptr, turned, partner, t, y);
-            if (dst != nullptr && here && h < h1) store8(dst + tok * ldo + (int64_t)h * D + ch, y);
-        }
-        if constexpr (kWhat != 0) {
-            if (cached) quantize_row<D>(a, y, slot, live && h < h1, h < heads ? h : 0, kWhat == 2);
+            for (int b = 0; b < kBatch; ++b) {
+                const int h = head_of(hb + (kBatch + b) * step);
+                load8(src + (int64_t)(h < heads ? h : heads - 1) * D, next[b]);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = next[j];
+        for (int b = 0; b < kBatch; ++b) {
+            if (hb + b * step >= h1) break;
+            const int h = head_of(hb + b * step);
+            R y[8];
+            if constexpr (kWhat == 2) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = (R)x[b][j];
+            } else {
+                norm_and_turn<D>(a, x[b], norm != nullptr, partner, t, y);
+                if (dst != nullptr && here && h < h1) store8(dst + tok * ldo + (int64_t)h * D + ch, y);
+            }
+            if constexpr (kWhat != 0) {
+                if (cached) quantize_row<D>(a, y, slot, live && h < h1, h < heads ? h : 0, kWhat == 2);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[b][j] = next[b][j];
     }
 }
 
@@ -345,33 +352,59 @@ __device__ __forceinline__ void hadamard_digits(half2v (&v)[4]) {
 #undef ITQ3S_STAGE
 }
 
-// A workgroup reads 32 listed rows of one head.  Key words go straight to their lanes; value bytes, which lie eight tokens
-// beside each other, are gathered token-fastest (neighbouring slots: neighbouring bytes) and turned round in LDS.
+// Eight digits' sums times a factor, rounded once to the type (fp16: by the instruction that multiplies).
+__device__ __forceinline__ void store_scaled(_Float16* p, const half2v (&v)[4], float f) {
+    half8 h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (_Float16)__builtin_fmaf((float)v[j >> 1][j & 1], f, 0.f);
+    *reinterpret_cast<half8*>(p) = h;
+}
+__device__ __forceinline__ void store_scaled(float* p, const half2v (&v)[4], float f) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        reinterpret_cast<floatx4*>(p)[i] = floatx4{(float)v[2 * i][0] * f, (float)v[2 * i][1] * f, (float)v[2 * i + 1][0] * f, (float)v[2 * i + 1][1] * f};
+}
+
+// Value bytes of a row's eight channels from `lane`'s first, as four words of two digits (to shift): the byte of channel c and of
+// c + 16 is one.
+__device__ __forceinline__ void value_pairs(const unsigned char* at, int shift, half2v (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = low_pair((((uint32_t)at[32 * j] | (uint32_t)at[32 * j + 16] << 16) >> shift) & 0x000f000fu);
+}
+
+// A workgroup reads 32 listed rows of one head.  Key words go straight to their lanes; of the values, whose bytes lie eight
+// tokens beside each other, whole blocks go through LDS: listed rows are mostly neighbours, so 32 of them lie in one block or
+// two.  Where they do not, a lane gathers its eight bytes from memory.
 template <int D, typename Out>
 __global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
-    constexpr int kRows = Rows<D>::kRows, kPitch = D / 2 + 8;
-    __shared__ __align__(16) unsigned char turn_round[32 * kPitch];
+    constexpr int kRows = Rows<D>::kRows, kChunks = D, kHalf = 1024 + 64;  // 16-byte chunks of a block's values; LDS bytes of 64 channels
+    __shared__ __align__(16) unsigned char values[2 * (D / 64) * kHalf];
     const int head = blockIdx.y;
     const int64_t first = (int64_t)blockIdx.x * 32;
-    const int tid = threadIdx.x, wave = tid >> 6;
-    {
-        const int i = tid & 31;
-        const int64_t token = first + i;
-        int64_t slot = token < a.T ? a.slots[token] : -1;
-        const bool live = slot >= 0 && slot < a.slots_end;
-        if (slot >= a.slots_end && tid < 32 && head == 0 && a.flags != nullptr) atomicOr(a.flags, kFlagBadSlot);
-        if (!live) slot = 0;
-        const int64_t block = slot >> 5;
-        const unsigned char* const at = a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks)) + 16 * D;
-        const int t = (int)(slot & 31);
-        unsigned char got[D / 16];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = lane_id();
+    auto place_of = [&](int64_t block) {
+        return a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks));
+    };
+    // every wavefront looks over the list (the lower half of its lanes does)
+    const int64_t mine = first + (lane & 31);
+    const int64_t listed = mine < a.T ? a.slots[mine] : -1;
+    const bool ours = listed >= 0 && listed < a.slots_end;
+    if (listed >= a.slots_end && tid < 32 && head == 0 && a.flags != nullptr) atomicOr(a.flags, kFlagBadSlot);
+    const int64_t my_block = ours ? listed >> 5 : -1;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(ours);
+    int64_t two[2] = {0, 0};
+    two[0] = two[1] = some != 0 ? __shfl(my_block, __builtin_ctzll(some), 64) : 0;
+    const uint64_t others = __builtin_amdgcn_ballot_w64(ours && my_block != two[0]);
+    if (others != 0) two[1] = __shfl(my_block, __builtin_ctzll(others), 64);
+    const bool near = __builtin_amdgcn_ballot_w64(ours && my_block != two[0] && my_block != two[1]) == 0;
+    if (near) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const int b = (tid >> 5) + 8 * k;  // byte p * 16 + c of the token
-            got[k] = at[value_byte(t, b >> 4, b & 15)];
+        for (int u = 0; u < 2 * kChunks / 256 + (kChunks < 128 ? 1 : 0); ++u) {
+            const int x = tid + 256 * u, which = x / kChunks, chunk = x % kChunks;
+            if (which == 0 || (which == 1 && others != 0))
+                *reinterpret_cast<u32x4*>(values + which * (D / 64) * kHalf + chunk / 64 * kHalf + chunk % 64 * 16) =
+                    reinterpret_cast<const u32x4*>(place_of(two[which == 0 ? 0 : 1]) + 16 * D)[chunk];
         }
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) turn_round[i * kPitch + (tid >> 5) + 8 * k] = got[k];
     }
     __syncthreads();
     const int row = Rows<D>::row(), ch = Rows<D>::channel();
@@ -380,33 +413,26 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
         const int i = wave * 8 + r0 + row;
         const int64_t token = first + i;
         const bool here = token < a.T;
-        int64_t slot = here ? a.slots[token] : -1;
+        int64_t slot = __shfl(listed, i, 64);
         const bool live = slot >= 0 && slot < a.slots_end;
-        if (!live) slot = 0;
+        if (!live) slot = near ? two[0] << 5 : 0;
         const int t = (int)(slot & 31);
         const int64_t block = slot >> 5;
-        const unsigned char* const base = a.data + block_offset<D>(block / a.page_blocks, head, a.kv_heads, a.page_blocks, (int)(block % a.page_blocks));
+        const unsigned char* const base = place_of(block);
         const uint32_t kw = *reinterpret_cast<const uint32_t*>(base + t * (D / 2) + ch / 2);
         const uint32_t steps = *reinterpret_cast<const uint32_t*>(base + 32 * D + 4 * t);
-        const u32x2 vb = *reinterpret_cast<const u32x2*>(turn_round + i * kPitch + (ch / 32) * 16 + (ch & 8));
-        const int shift = (ch & 16) != 0 ? 4 : 0;
+        const int byte = value_byte(t, ch / 32, ch & 8), shift = (ch & 16) != 0 ? 4 : 0;
         half2v k[4] = {low_pair(kw), high_pair(kw), low_pair(kw >> 8), high_pair(kw >> 8)};
         half2v v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t w = vb[j >> 1] >> ((j & 1) * 16 + shift);
-            v[j] = low_pair((w & 15u) | ((w & 0x0f00u) << 8));
-        }
+        if (near) value_pairs(values + (block == two[0] ? 0 : (D / 64) * kHalf) + byte / 1024 * kHalf + byte % 1024, shift, v);
+        else value_pairs(base + 16 * D + byte, shift, v);
         hadamard_digits<D>(k);
         hadamard_digits<D>(v);
         const float root = (float)(1.0 / kRootD<D>);
         const float ks = live ? f16_bits_to_f32(steps & 0xffffu) * root : 0.f, vs = live ? f16_bits_to_f32(steps >> 16) * root : 0.f;
         if (here) {
-            float kf[8], vf[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) kf[j] = live ? (float)k[j >> 1][j & 1] * ks : 0.f, vf[j] = live ? (float)v[j >> 1][j & 1] * vs : 0.f;
-            store8(static_cast<Out*>(a.K) + token * a.ldk + (int64_t)head * D + ch, kf);
-            store8(static_cast<Out*>(a.V) + token * a.ldv + (int64_t)head * D + ch, vf);
+            store_scaled(static_cast<Out*>(a.K) + token * a.ldk + (int64_t)head * D + ch, k, ks);
+            store_scaled(static_cast<Out*>(a.V) + token * a.ldv + (int64_t)head * D + ch, v, vs);
         }
     }
 }
