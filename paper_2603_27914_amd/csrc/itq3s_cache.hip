@@ -10,10 +10,10 @@
 // library's sine: with 32 bits some 1e-6 of the digits fall on the other side of their border.  Queries, which are
 // only rounded, take 32 bits behind a 64-bit angle.
 //
-// A lane holds eight channels of a row: 8, 16 or 32 lanes a row, 8, 4 or 2 rows a wavefront, the rows of one wavefront
-// neighbouring tokens (so that their value bytes share words of memory) or, where there are few tokens, heads of a token.
-// It computes the sines of its channels once and walks over heads with them.  Everything is bound by memory: append
-// moves 2 or 4 bytes a value in and out, read 4.1 bits in and 2 or 4 bytes out.
+// A lane holds eight channels of a row: 8, 16 or 32 lanes a row, 8, 4 or 2 rows a wavefront.  The rows of one wavefront are heads of
+// one token (queries: a kilobyte of neighbouring memory an instruction; they share the sines, so each row of lanes works
+// out its part of them) or, for keys and values where there are many tokens, neighbouring tokens (so that their value
+// bytes share words of memory).  A wavefront walks over heads with the sines that it has worked out once.
 #include <type_traits>
 
 #include "itq3s_attention.h"
@@ -84,9 +84,9 @@ struct AppendArgs {
     int q_heads, kv_heads, rot, interleaved;
     float eps, gain;
     int page_blocks;                  // blocks of 32 tokens a page
-    int tokens;                       // neighbouring tokens in a wavefront (1 or as many as it has rows)
+    int tokens;                       // of keys and values: neighbouring tokens in a wavefront (1 or as many as it has rows)
     int q_step, kv_step;              // heads that a wavefront walks over
-    int64_t groups;                   // token groups
+    int64_t groups;                   // groups of tokens for keys and values (queries: every token is one)
     int64_t k_jobs, v_jobs, q_jobs;   // wavefronts
 };
 
@@ -103,8 +103,8 @@ template <typename R>
 struct Turns {
     R own[8], other[8];
 };
-template <typename R>
-__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, int ch, bool turned, const float* norm, Turns<R>& t) {
+template <int D, typename R>
+__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, bool by_token, int ch, bool turned, const float* norm, Turns<R>& t) {
     const int half = a.rot / 2;
     const bool upper = ch >= half;
     const int mate = turned && !a.interleaved ? (upper ? ch - half : ch + half) : ch;
@@ -116,16 +116,45 @@ __device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, i
         load8(norm + mate, wm);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t.own[j] = (R)w[j], t.other[j] = (R)0;
-    if (!turned) return;
-    const double pos = (double)a.positions[token], gain = (double)a.gain;
-    double c = 0.0, s = 0.0;
+    for (int j = 0; j < 8; ++j) t.own[j] = (R)1, t.other[j] = (R)0;
+    if (a.rot != 0) {
+        const double pos = (double)a.positions[token], gain = (double)a.gain;
+        const int first = !turned ? 0 : a.interleaved ? ch / 2 : upper ? ch - half : ch;  // (lanes that do not turn work on a frequency that is there)
+        double c = 0.0, s = 0.0;
+        if (by_token) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (j % 2 == 0 || !a.interleaved) turn(pos * a.freq[a.interleaved ? (ch + j) / 2 : (upper ? ch - half : ch) + j], c, s);
-        const bool second = a.interleaved ? j % 2 == 1 : upper;  // of its pair
-        t.own[j] = (R)(c * gain * (double)w[j]);
-        t.other[j] = (R)((second ? s : -s) * gain * (double)(a.interleaved ? w[j ^ 1] : wm[j]));
+            for (int j = 0; j < 8; ++j) {
+                if (j % 2 == 0 || !a.interleaved) turn(pos * a.freq[first + (a.interleaved ? j / 2 : j)], c, s);
+                t.own[j] = (R)(c * gain), t.other[j] = (R)(s * gain);
+            }
+        } else {  // the rows of lanes have a token in common, and the same channels: each works out a part
+            constexpr int kPart = 8 / Rows<D>::kRows;
+            R pc[kPart], ps[kPart];
+#pragma unroll
+            for (int j = 0; j < kPart; ++j) {
+                const int k = Rows<D>::row() * kPart + j;
+                turn(pos * a.freq[first + (a.interleaved ? k / 2 : k)], c, s);
+                pc[j] = (R)(c * gain), ps[j] = (R)(s * gain);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int from = j / kPart * Rows<D>::kLanes + lane_id() % Rows<D>::kLanes;
+                t.own[j] = __shfl(pc[j % kPart], from, 64), t.other[j] = __shfl(ps[j % kPart], from, 64);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool second = a.interleaved ? j % 2 == 1 : upper;  // of its pair
+            t.other[j] = !turned ? (R)0 : second ? t.other[j] : -t.other[j];
+            t.own[j] = turned ? t.own[j] : (R)1;
+        }
+    }
+    if (norm != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            t.own[j] = t.own[j] * (R)w[j];
+            t.other[j] = t.other[j] * (R)(a.interleaved ? w[j ^ 1] : wm[j]);
+        }
     }
 }
 
@@ -187,16 +216,28 @@ __device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8]
     if (bad) s = (_Float16)0.f;
     const double step = (double)(float)s * kRootD<D>, inv = step > 0.0 ? 1.0 / step : 0.0;
     int d[8];
+    // The nearest whole number, from the low bits of w / step + 1.5 2^52; it is right where the remainder stays clear of half a step.
+    constexpr double kWhole = 6755399441055744.0;
+    double rest = 0.0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        // floor(w / step + 1/2): by the reciprocal, then set right by the remainder, whose sign is exact
-        double q = __builtin_floor(__builtin_fma(v[j], inv, 0.5));
-        const double rest = __builtin_fma(-q, step, v[j]);
-        if (rest >= 0.5 * step) q += 1.0;
-        if (rest < -0.5 * step) q -= 1.0;
-        q = __builtin_fmin(__builtin_fmax(q, -8.0), 7.0);
-        d[j] = step > 0.0 ? (int)q + 8 : 8;
+        const double q = __builtin_fma(v[j], inv, kWhole);
+        rest = __builtin_fmax(rest, __builtin_fabs(__builtin_fma(kWhole - q, step, v[j])));
+        d[j] = __double2loint(q);
     }
+    if (__builtin_amdgcn_ballot_w64(!(rest < step * (0.5 - 0x1p-40))) != 0) {  // a border (or a step of 0) in the wavefront
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // floor(w / step + 1/2): by the reciprocal, then set right by the remainder, whose sign is exact
+            double q = __builtin_floor(__builtin_fma(v[j], inv, 0.5));
+            const double r = __builtin_fma(-q, step, v[j]);
+            if (r >= 0.5 * step) q += 1.0;
+            if (r < -0.5 * step) q -= 1.0;
+            d[j] = step > 0.0 ? (int)__builtin_fmin(__builtin_fmax(q, -8.0), 7.0) : 0;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d[j] = (d[j] < -8 ? -8 : d[j] > 7 ? 7 : d[j]) + 8;
     const int lane = lane_id(), ch = Rows<D>::channel();
     if (a.flags != nullptr && live && ch == 0 && (bad || sat)) atomicOr(a.flags, bad ? kFlagNonFinite : kFlagScaleSat);
     const int t = (int)(slot & 31);
@@ -230,7 +271,7 @@ template <int D, typename In, typename Out, int kWhat>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, int h0, int h1) {
     typedef typename std::conditional<kWhat == 0, float, double>::type R;
     const int row = Rows<D>::row(), ch = Rows<D>::channel();
-    const bool by_token = a.tokens > 1;
+    const bool by_token = kWhat != 0 && a.tokens > 1;
     const int64_t token = by_token ? group * Rows<D>::kRows + row : group;
     const bool here = token < a.T;
     const int64_t tok = here ? token : a.T - 1;
@@ -263,7 +304,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, 
     const int partner = lane_id() + (turned ? (ch < half ? half : -half) : 0) / 8;
     const float* const norm = kWhat == 0 ? a.q_norm : kWhat == 1 ? a.k_norm : nullptr;
     Turns<R> t;
-    if constexpr (kWhat != 2) find_turns<R>(a, tok, ch, turned, norm, t);
+    if constexpr (kWhat != 2) find_turns<D, R>(a, tok, by_token, ch, turned, norm, t);
     for (int hb = h0; hb < h1; hb += kBatch * step) {
         if (hb + kBatch * step < h1) {
 #pragma unroll
@@ -311,8 +352,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
     }
     job -= a.v_jobs;
     if (job < a.q_jobs) {
-        const int h0 = (int)(job / a.groups) * a.q_step;
-        append_rows<D, In, Out, 0>(a, job % a.groups, h0, h0 + a.q_step < a.q_heads ? h0 + a.q_step : a.q_heads);
+        const int h0 = (int)(job / a.T) * a.q_step;
+        append_rows<D, In, Out, 0>(a, job % a.T, h0, h0 + a.q_step < a.q_heads ? h0 + a.q_step : a.q_heads);
     }
 }
 
@@ -459,19 +500,18 @@ int launch_append(const AppendCall& c, hipStream_t st) {
     a.q_heads = c.Q != nullptr ? c.q_heads : 0, a.kv_heads = c.kv_heads, a.rot = c.rot, a.interleaved = c.interleaved, a.eps = c.eps, a.gain = c.gain;
     a.data = c.cache.data, a.page_blocks = c.cache.data != nullptr ? c.cache.page_blocks : 1;
     a.slots_end = c.cache.data != nullptr ? c.cache.pages * c.cache.page_blocks * kCacheBlock : 0;
-    // Neighbouring tokens in a wavefront where that leaves every compute unit four of them, else heads of one token.
+    // Keys and values: neighbouring tokens in a wavefront where that leaves every compute unit four of them.
     a.tokens = c.T * c.kv_heads / rows >= 4 * (int64_t)cu_count() ? rows : 1;
     a.groups = (c.T + a.tokens - 1) / a.tokens;
     // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  16 a unit are plenty.
-    auto heads_of = [&](int heads) {
-        int step = a.tokens > 1 ? 1 : rows;
-        while (step < heads && a.groups * ((heads + 2 * step - 1) / (2 * step)) >= 16 * (int64_t)cu_count()) step *= 2;
+    auto heads_of = [&](int heads, int step, int64_t groups) {
+        while (step < heads && groups * ((heads + 2 * step - 1) / (2 * step)) >= 16 * (int64_t)cu_count()) step *= 2;
         return step;
     };
-    a.q_step = heads_of(a.q_heads), a.kv_step = heads_of(c.kv_heads);
+    a.q_step = heads_of(a.q_heads, rows, c.T), a.kv_step = heads_of(c.kv_heads, a.tokens > 1 ? 1 : rows, a.groups);
     a.k_jobs = c.K != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
     a.v_jobs = c.V != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
-    a.q_jobs = a.q_heads > 0 ? a.groups * ((a.q_heads + a.q_step - 1) / a.q_step) : 0;
+    a.q_jobs = a.q_heads > 0 ? c.T * ((a.q_heads + a.q_step - 1) / a.q_step) : 0;
     const int64_t blocks = (a.k_jobs + a.v_jobs + a.q_jobs + 3) / 4;
     if (blocks > 0x7fffffffLL) return -2;
     if (c.head_dim == 64) return start_append<64>(a, blocks, c.in_f16, c.out_f16, st);
