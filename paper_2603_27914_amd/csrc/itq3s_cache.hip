@@ -11,9 +11,9 @@
 // only rounded, take 32 bits behind a 64-bit angle.
 //
 // A lane holds eight channels of a row: 8, 16 or 32 lanes a row, 8, 4 or 2 rows a wavefront.  The rows of one wavefront are heads of
-// one token (queries: a kilobyte of neighbouring memory an instruction; they share the sines, so each row of lanes works
-// out its part of them) or, for keys and values where there are many tokens, neighbouring tokens (so that their value
-// bytes share words of memory).  A wavefront walks over heads with the sines that it has worked out once.
+// one token (a kilobyte of neighbouring memory an instruction; they share the sines, so each row of lanes works out its
+// part of them) or, for values where there are many tokens, neighbouring tokens (so that their bytes share words of
+// memory).  A wavefront walks over heads with the sines that it has worked out once.
 #include <type_traits>
 
 #include "itq3s_attention.h"
@@ -84,10 +84,11 @@ struct AppendArgs {
     int q_heads, kv_heads, rot, interleaved;
     float eps, gain;
     int page_blocks;                  // blocks of 32 tokens a page
-    int tokens;                       // of keys and values: neighbouring tokens in a wavefront (1 or as many as it has rows)
-    int q_step, kv_step;              // heads that a wavefront walks over
-    int64_t groups;                   // groups of tokens for keys and values (queries: every token is one)
+    int tokens;                       // of values: neighbouring tokens in a wavefront (1 or as many as it has rows)
+    int q_step, k_step, v_step;       // heads that a wavefront walks over
+    int64_t groups;                   // groups of tokens for values (else every token is one)
     int64_t k_jobs, v_jobs, q_jobs;   // wavefronts
+    int few_are_kv, few_blocks, period;  // workgroups of keys and values (or of queries), one among so many while there are any
 };
 
 template <int D>
@@ -104,7 +105,7 @@ struct Turns {
     R own[8], other[8];
 };
 template <int D, typename R>
-__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, bool by_token, int ch, bool turned, const float* norm, Turns<R>& t) {
+__device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, int ch, bool turned, const float* norm, Turns<R>& t) {
     const int half = a.rot / 2;
     const bool upper = ch >= half;
     const int mate = turned && !a.interleaved ? (upper ? ch - half : ch + half) : ch;
@@ -120,27 +121,20 @@ __device__ __forceinline__ void find_turns(const AppendArgs& a, int64_t token, b
     if (a.rot != 0) {
         const double pos = (double)a.positions[token], gain = (double)a.gain;
         const int first = !turned ? 0 : a.interleaved ? ch / 2 : upper ? ch - half : ch;  // (lanes that do not turn work on a frequency that is there)
-        double c = 0.0, s = 0.0;
-        if (by_token) {
+        // the rows of lanes have a token in common, and the same channels: each works out a part
+        constexpr int kPart = 8 / Rows<D>::kRows;
+        R pc[kPart], ps[kPart];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j % 2 == 0 || !a.interleaved) turn(pos * a.freq[first + (a.interleaved ? j / 2 : j)], c, s);
-                t.own[j] = (R)(c * gain), t.other[j] = (R)(s * gain);
-            }
-        } else {  // the rows of lanes have a token in common, and the same channels: each works out a part
-            constexpr int kPart = 8 / Rows<D>::kRows;
-            R pc[kPart], ps[kPart];
+        for (int j = 0; j < kPart; ++j) {
+            const int k = Rows<D>::row() * kPart + j;
+            double c, s;
+            turn(pos * a.freq[first + (a.interleaved ? k / 2 : k)], c, s);
+            pc[j] = (R)(c * gain), ps[j] = (R)(s * gain);
+        }
 #pragma unroll
-            for (int j = 0; j < kPart; ++j) {
-                const int k = Rows<D>::row() * kPart + j;
-                turn(pos * a.freq[first + (a.interleaved ? k / 2 : k)], c, s);
-                pc[j] = (R)(c * gain), ps[j] = (R)(s * gain);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int from = j / kPart * Rows<D>::kLanes + lane_id() % Rows<D>::kLanes;
-                t.own[j] = __shfl(pc[j % kPart], from, 64), t.other[j] = __shfl(ps[j % kPart], from, 64);
-            }
+        for (int j = 0; j < 8; ++j) {
+            const int from = j / kPart * Rows<D>::kLanes + lane_id() % Rows<D>::kLanes;
+            t.own[j] = __shfl(pc[j % kPart], from, 64), t.other[j] = __shfl(ps[j % kPart], from, 64);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -271,7 +265,7 @@ template <int D, typename In, typename Out, int kWhat>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, int h0, int h1) {
     typedef typename std::conditional<kWhat == 0, float, double>::type R;
     const int row = Rows<D>::row(), ch = Rows<D>::channel();
-    const bool by_token = kWhat != 0 && a.tokens > 1;
+    const bool by_token = kWhat == 2 && a.tokens > 1;
     const int64_t token = by_token ? group * Rows<D>::kRows + row : group;
     const bool here = token < a.T;
     const int64_t tok = here ? token : a.T - 1;
@@ -304,7 +298,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, 
     const int partner = lane_id() + (turned ? (ch < half ? half : -half) : 0) / 8;
     const float* const norm = kWhat == 0 ? a.q_norm : kWhat == 1 ? a.k_norm : nullptr;
     Turns<R> t;
-    if constexpr (kWhat != 2) find_turns<D, R>(a, tok, by_token, ch, turned, norm, t);
+    if constexpr (kWhat != 2) find_turns<D, R>(a, tok, ch, turned, norm, t);
     for (int hb = h0; hb < h1; hb += kBatch * step) {
         if (hb + kBatch * step < h1) {
 #pragma unroll
@@ -338,22 +332,29 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, 
 
 template <int D, typename In, typename Out>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
-    int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // Workgroups of keys and values, which compute, and of queries, which move memory, run side by side: the fewer ones are spread
+    // among the others.
+    const int b = blockIdx.x, turn = b / a.period, before = turn + (b % a.period != 0 ? 1 : 0);
+    const bool few = b % a.period == 0 && turn < a.few_blocks, kv = few == (a.few_are_kv != 0);
+    const int64_t block = few ? turn : b - (before < a.few_blocks ? before : a.few_blocks);
+    int64_t job = block * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (!kv) {
+        if (job < a.q_jobs) {
+            const int h0 = (int)(job / a.T) * a.q_step;
+            append_rows<D, In, Out, 0>(a, job % a.T, h0, h0 + a.q_step < a.q_heads ? h0 + a.q_step : a.q_heads);
+        }
+        return;
+    }
     if (job < a.k_jobs) {
-        const int h0 = (int)(job / a.groups) * a.kv_step;
-        append_rows<D, In, Out, 1>(a, job % a.groups, h0, h0 + a.kv_step < a.kv_heads ? h0 + a.kv_step : a.kv_heads);
+        const int h0 = (int)(job / a.T) * a.k_step;
+        append_rows<D, In, Out, 1>(a, job % a.T, h0, h0 + a.k_step < a.kv_heads ? h0 + a.k_step : a.kv_heads);
         return;
     }
     job -= a.k_jobs;
     if (job < a.v_jobs) {
-        const int h0 = (int)(job / a.groups) * a.kv_step;
-        append_rows<D, In, Out, 2>(a, job % a.groups, h0, h0 + a.kv_step < a.kv_heads ? h0 + a.kv_step : a.kv_heads);
+        const int h0 = (int)(job / a.groups) * a.v_step;
+        append_rows<D, In, Out, 2>(a, job % a.groups, h0, h0 + a.v_step < a.kv_heads ? h0 + a.v_step : a.kv_heads);
         return;
-    }
-    job -= a.v_jobs;
-    if (job < a.q_jobs) {
-        const int h0 = (int)(job / a.T) * a.q_step;
-        append_rows<D, In, Out, 0>(a, job % a.T, h0, h0 + a.q_step < a.q_heads ? h0 + a.q_step : a.q_heads);
     }
 }
 
@@ -398,12 +399,12 @@ __device__ __forceinline__ void store_scaled(_Float16* p, const half2v (&v)[4], 
     half8 h;
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = (_Float16)__builtin_fmaf((float)v[j >> 1][j & 1], f, 0.f);
-    *reinterpret_cast<half8*>(p) = h;
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, h), reinterpret_cast<u32x4*>(p));
 }
 __device__ __forceinline__ void store_scaled(float* p, const half2v (&v)[4], float f) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        reinterpret_cast<floatx4*>(p)[i] = floatx4{(float)v[2 * i][0] * f, (float)v[2 * i][1] * f, (float)v[2 * i + 1][0] * f, (float)v[2 * i + 1][1] * f};
+        __builtin_nontemporal_store(floatx4{(float)v[2 * i][0] * f, (float)v[2 * i][1] * f, (float)v[2 * i + 1][0] * f, (float)v[2 * i + 1][1] * f}, reinterpret_cast<floatx4*>(p) + i);
 }
 
 // Value bytes of a row's eight channels from `lane`'s first, as four words of two digits (to shift): the byte of channel c and of
@@ -438,40 +439,51 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
     const uint64_t others = __builtin_amdgcn_ballot_w64(ours && my_block != two[0]);
     if (others != 0) two[1] = __shfl(my_block, __builtin_ctzll(others), 64);
     const bool near = __builtin_amdgcn_ballot_w64(ours && my_block != two[0] && my_block != two[1]) == 0;
+    // a lane's rows, and what of them does not go through LDS
+    constexpr int kRounds = 8 / kRows;
+    const int row = Rows<D>::row(), ch = Rows<D>::channel();
+    uint32_t kw[kRounds], steps[kRounds];
+    int at[kRounds];  // its value bytes in LDS
+    bool live[kRounds];
+#pragma unroll
+    for (int n = 0; n < kRounds; ++n) {
+        int64_t slot = __shfl(listed, wave * 8 + n * kRows + row, 64);
+        live[n] = slot >= 0 && slot < a.slots_end;
+        if (!live[n]) slot = two[0] << 5;
+        const int t = (int)(slot & 31), byte = value_byte(t, ch / 32, ch & 8);
+        const unsigned char* const base = place_of(slot >> 5);
+        kw[n] = *reinterpret_cast<const uint32_t*>(base + t * (D / 2) + ch / 2);
+        steps[n] = *reinterpret_cast<const uint32_t*>(base + 32 * D + 4 * t);
+        at[n] = ((slot >> 5) == two[0] ? 0 : (D / 64) * kHalf) + byte / 1024 * kHalf + byte % 1024;
+    }
     if (near) {
 #pragma unroll
-        for (int u = 0; u < 2 * kChunks / 256 + (kChunks < 128 ? 1 : 0); ++u) {
+        for (int u = 0; u < (2 * kChunks + 255) / 256; ++u) {
             const int x = tid + 256 * u, which = x / kChunks, chunk = x % kChunks;
             if (which == 0 || (which == 1 && others != 0))
                 *reinterpret_cast<u32x4*>(values + which * (D / 64) * kHalf + chunk / 64 * kHalf + chunk % 64 * 16) =
-                    reinterpret_cast<const u32x4*>(place_of(two[which == 0 ? 0 : 1]) + 16 * D)[chunk];
+                    reinterpret_cast<const u32x4*>(place_of(which == 0 ? two[0] : two[1]) + 16 * D)[chunk];
         }
     }
     __syncthreads();
-    const int row = Rows<D>::row(), ch = Rows<D>::channel();
 #pragma unroll
-    for (int r0 = 0; r0 < 8; r0 += kRows) {
-        const int i = wave * 8 + r0 + row;
+    for (int n = 0; n < kRounds; ++n) {
+        const int i = wave * 8 + n * kRows + row, shift = (ch & 16) != 0 ? 4 : 0;
         const int64_t token = first + i;
-        const bool here = token < a.T;
-        int64_t slot = __shfl(listed, i, 64);
-        const bool live = slot >= 0 && slot < a.slots_end;
-        if (!live) slot = near ? two[0] << 5 : 0;
-        const int t = (int)(slot & 31);
-        const int64_t block = slot >> 5;
-        const unsigned char* const base = place_of(block);
-        const uint32_t kw = *reinterpret_cast<const uint32_t*>(base + t * (D / 2) + ch / 2);
-        const uint32_t steps = *reinterpret_cast<const uint32_t*>(base + 32 * D + 4 * t);
-        const int byte = value_byte(t, ch / 32, ch & 8), shift = (ch & 16) != 0 ? 4 : 0;
-        half2v k[4] = {low_pair(kw), high_pair(kw), low_pair(kw >> 8), high_pair(kw >> 8)};
+        half2v k[4] = {low_pair(kw[n]), high_pair(kw[n]), low_pair(kw[n] >> 8), high_pair(kw[n] >> 8)};
         half2v v[4];
-        if (near) value_pairs(values + (block == two[0] ? 0 : (D / 64) * kHalf) + byte / 1024 * kHalf + byte % 1024, shift, v);
-        else value_pairs(base + 16 * D + byte, shift, v);
+        if (near) {
+            value_pairs(values + at[n], shift, v);
+        } else {
+            int64_t slot = __shfl(listed, i, 64);  // (all lanes: a row's entry may be with one of a row that is not there)
+            if (!live[n]) slot = two[0] << 5;
+            value_pairs(place_of(slot >> 5) + 16 * D + value_byte((int)(slot & 31), ch / 32, ch & 8), shift, v);
+        }
         hadamard_digits<D>(k);
         hadamard_digits<D>(v);
         const float root = (float)(1.0 / kRootD<D>);
-        const float ks = live ? f16_bits_to_f32(steps & 0xffffu) * root : 0.f, vs = live ? f16_bits_to_f32(steps >> 16) * root : 0.f;
-        if (here) {
+        const float ks = live[n] ? f16_bits_to_f32(steps[n] & 0xffffu) * root : 0.f, vs = live[n] ? f16_bits_to_f32(steps[n] >> 16) * root : 0.f;
+        if (token < a.T) {
             store_scaled(static_cast<Out*>(a.K) + token * a.ldk + (int64_t)head * D + ch, k, ks);
             store_scaled(static_cast<Out*>(a.V) + token * a.ldv + (int64_t)head * D + ch, v, vs);
         }
@@ -500,20 +512,23 @@ int launch_append(const AppendCall& c, hipStream_t st) {
     a.q_heads = c.Q != nullptr ? c.q_heads : 0, a.kv_heads = c.kv_heads, a.rot = c.rot, a.interleaved = c.interleaved, a.eps = c.eps, a.gain = c.gain;
     a.data = c.cache.data, a.page_blocks = c.cache.data != nullptr ? c.cache.page_blocks : 1;
     a.slots_end = c.cache.data != nullptr ? c.cache.pages * c.cache.page_blocks * kCacheBlock : 0;
-    // Keys and values: neighbouring tokens in a wavefront where that leaves every compute unit four of them.
+    // Values: neighbouring tokens in a wavefront where that leaves every compute unit four of them.
     a.tokens = c.T * c.kv_heads / rows >= 4 * (int64_t)cu_count() ? rows : 1;
     a.groups = (c.T + a.tokens - 1) / a.tokens;
-    // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  16 a unit are plenty.
-    auto heads_of = [&](int heads, int step, int64_t groups) {
-        while (step < heads && groups * ((heads + 2 * step - 1) / (2 * step)) >= 16 * (int64_t)cu_count()) step *= 2;
+    // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  16 a unit are plenty, and 32
+    // of the short ones of values (11385 tokens, 64 and 8 heads of 128: 8, 4, 2 and 1 heads 116, 114, 106 and 118 us).
+    auto heads_of = [&](int heads, int step, int64_t groups, int plenty) {
+        while (step < heads && groups * ((heads + 2 * step - 1) / (2 * step)) >= plenty * (int64_t)cu_count()) step *= 2;
         return step;
     };
-    a.q_step = heads_of(a.q_heads, rows, c.T), a.kv_step = heads_of(c.kv_heads, a.tokens > 1 ? 1 : rows, a.groups);
-    a.k_jobs = c.K != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
-    a.v_jobs = c.V != nullptr ? a.groups * ((c.kv_heads + a.kv_step - 1) / a.kv_step) : 0;
+    a.q_step = heads_of(a.q_heads, rows, c.T, 16), a.k_step = heads_of(c.kv_heads, rows, c.T, 16), a.v_step = heads_of(c.kv_heads, a.tokens > 1 ? 1 : rows, a.groups, 32);
+    a.k_jobs = c.K != nullptr ? c.T * ((c.kv_heads + a.k_step - 1) / a.k_step) : 0;
+    a.v_jobs = c.V != nullptr ? a.groups * ((c.kv_heads + a.v_step - 1) / a.v_step) : 0;
     a.q_jobs = a.q_heads > 0 ? c.T * ((a.q_heads + a.q_step - 1) / a.q_step) : 0;
-    const int64_t blocks = (a.k_jobs + a.v_jobs + a.q_jobs + 3) / 4;
+    const int64_t kv_blocks = (a.k_jobs + a.v_jobs + 3) / 4, q_blocks = (a.q_jobs + 3) / 4, blocks = kv_blocks + q_blocks;
     if (blocks > 0x7fffffffLL) return -2;
+    a.few_are_kv = kv_blocks <= q_blocks, a.few_blocks = (int)(a.few_are_kv ? kv_blocks : q_blocks);
+    a.period = a.few_blocks > 0 ? (int)(blocks / a.few_blocks) : 1;
     if (c.head_dim == 64) return start_append<64>(a, blocks, c.in_f16, c.out_f16, st);
     if (c.head_dim == 128) return start_append<128>(a, blocks, c.in_f16, c.out_f16, st);
     return start_append<256>(a, blocks, c.in_f16, c.out_f16, st);
