@@ -276,7 +276,7 @@ int itq3s_rope_frequencies(int rot, double base, double factor, int64_t trained_
  *   norm (q_norm, k_norm not NULL)  x * w / sqrt(mean(x^2) + eps), w the head_dim weights, fp32, shared by the heads
  *   rotation (rot > 0)  pairs (x_a, x_b) of the first rot channels -- (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved --
  *                       become gain * (x_a cos - x_b sin, x_b cos + x_a sin), angle positions[t] * freq[i] in 64 bits
- * then Q_out and K_out receive the results (rounded once; each may be its input with the same stride), and the cache the
+ * then Q_out and K_out receive the results (rounded once; each may be its input, with the same stride and type, else overlaps nothing), and the cache the
  * codes of the rotated keys (unrounded) and of V at slots[t].
  *   Q      may be NULL: no queries (Q_out, q_heads unused)
  *   K      may be NULL where there is no cache;  K_out may be NULL where there is one
@@ -285,14 +285,15 @@ int itq3s_rope_frequencies(int rot, double base, double factor, int64_t trained_
  *   slots  device, T int64: where token t goes.  Negative: nowhere (padding; its Q_out and K_out are written all the same).  Beyond
  *          the cache: nowhere, ITQ3S_FLAG_BAD_SLOT.  Two tokens of one call at one slot leave there digits of either.
  *   positions device, T int32 (not needed if rot is 0);  freq device, rot / 2 doubles
- *   rot a multiple of 16, at most head_dim;  in_dtype of Q, K and V, out_dtype of Q_out and K_out;  T up to 2^31 - 1 */
+ *   rot a multiple of 16, at most head_dim;  in_dtype of Q, K and V, out_dtype of Q_out and K_out;  T up to 2^24
+ * Queries are computed in 32 bits behind their 64-bit angles (normed ones: mean squares within fp32's range), keys in 64. */
 int itq3s_cache_append(const void *Q, int64_t ldq, int q_heads, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int in_dtype,
                        int kv_heads, int head_dim, const float *q_norm, const float *k_norm, float eps, const int32_t *positions,
                        const double *freq, int rot, int interleaved, float gain, void *Q_out, int64_t ldqo, void *K_out, int64_t ldko,
                        int out_dtype, const itq3s_cache *cache, const int64_t *slots, uint32_t *status_flags, void *stream);
 
 /* Rows of the cache as the values that they stand for: K_out[t], V_out[t] (T x (kv_heads * head_dim) of out_dtype) of slots[t], in
- * any order, any number of times.  A negative slot gives zeros, one beyond the cache zeros and ITQ3S_FLAG_BAD_SLOT. */
+ * any order, any number of times, T up to 2^28.  A negative slot gives zeros, one beyond the cache zeros and ITQ3S_FLAG_BAD_SLOT. */
 int itq3s_cache_read(const itq3s_cache *cache, const int64_t *slots, int64_t T, void *K_out, int64_t ldk, void *V_out, int64_t ldv,
                      int out_dtype, uint32_t *status_flags, void *stream);
 
@@ -305,11 +306,11 @@ int itq3s_cache_read(const itq3s_cache *cache, const int64_t *slots, int64_t T, 
  *   Q, out   device, T x (q_heads * head_dim) fp16
  *   q_starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it);  kv_lens device, seqs int32 (negative: 0; more
  *            than ld_pages * page_tokens: that much, ITQ3S_FLAG_BAD_SLOT);  pages device, int32: a page that is not of
- *            the cache is taken for tokens that nobody sees, ITQ3S_FLAG_BAD_SLOT; entries behind a sequence's last token are not read
+ *            the cache is taken for tokens that nobody sees, ITQ3S_FLAG_BAD_SLOT; entries behind a sequence's last token may be anything
  *   max_q, max_kv  the most rows and tokens of a sequence that the work is cut up for.  Longer sequences are computed all the same,
  *            slower; with max_q above T, T is meant
- *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  |scale| up to 2^40
- *   workspace device, 256-byte aligned, itq3s_cache_attention_workspace_bytes() of the same sizes (never 0); as for itq3s_matmul */
+ *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs * kv_heads up to 2^22;  |scale| up to 2^40;  out overlaps no input
+ *   workspace device, 256-byte aligned, itq3s_cache_attention_workspace_bytes() of the same sizes on the same device (never 0); as for itq3s_matmul */
 size_t itq3s_cache_attention_workspace_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv);
 int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, const itq3s_cache *cache, const int32_t *q_starts,
                           const int32_t *kv_lens, int64_t seqs, const int32_t *pages, int64_t ld_pages, int64_t max_q, int64_t max_kv,
@@ -322,7 +323,7 @@ int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, co
  *   Q, out T x (q_heads * head_dim), K, V T x (kv_heads * head_dim), all fp16;  out must not overlap the inputs
  *   starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it)
  *   max_len  the most rows of a sequence that the work is cut up for (longer ones are computed all the same, slower)
- *   T * (q_heads / kv_heads) up to 2^30, seqs up to 2^24;  ldk and ldv up to 2^23;  |scale| up to 2^40;  no workspace */
+ *   T * (q_heads / kv_heads) up to 2^30, seqs * kv_heads up to 2^22;  ldk and ldv up to 2^23;  |scale| up to 2^40;  no workspace */
 int itq3s_prompt_attention(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T, int q_heads,
                            int kv_heads, int head_dim, const int32_t *starts, int64_t seqs, int64_t max_len, int causal, float scale,
                            void *out, int64_t ldo, void *stream);

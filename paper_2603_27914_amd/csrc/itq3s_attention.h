@@ -9,6 +9,14 @@ namespace itq3s {
 
 constexpr uint32_t kFlagBadSlot = 32u;
 
+// Attention: workgroups for `tiles` tiles of each of `units` heads of sequences.  A launch has less than 2^32 threads, and
+// estimates of a sequence's rows may be far too high: a workgroup takes several tiles where there would be too many.
+constexpr int64_t kMostUnits = 1LL << 22;
+inline int64_t most_tiles(int64_t tiles, int64_t units) {
+    const int64_t most = kMostUnits / units;
+    return tiles < most ? tiles : most;
+}
+
 struct CacheView {
     unsigned char* data;
     int64_t pages;

@@ -31,7 +31,8 @@ inline bool heads_ok(int q_heads, int kv_heads) {
     return q_heads > 0 && q_heads <= 65536 && kv_heads > 0 && kv_heads <= 1024 && q_heads % kv_heads == 0;
 }
 
-constexpr int64_t kMostRows = 1LL << 30, kMostSeqs = 1LL << 24, kMostBytes = 1LL << 48, kMostStride = 1LL << 23;
+constexpr int64_t kMostRows = 1LL << 30, kMostBytes = 1LL << 48, kMostStride = 1LL << 23;
+constexpr int64_t kMostAppended = 1LL << 24, kMostRead = 1LL << 28;  // tokens: a launch has less than 2^32 threads
 constexpr float kMostScale = 1099511627776.f;  // 2^40: scores stay within fp32
 
 }  // namespace
@@ -68,7 +69,7 @@ int itq3s_cache_append(const void* Q, int64_t ldq, int q_heads, const void* K, i
     if ((!Q && !K) || (Q && !Q_out) || (K && !K_out && !cache) || (V && !cache)) return ITQ3S_ERR_NULL;
     if (cache && (!K || !V || !slots)) return ITQ3S_ERR_NULL;
     if (rot != 0 && (!positions || !freq)) return ITQ3S_ERR_NULL;
-    if (T <= 0 || T > 0x7fffffffLL || !head_dim_ok(head_dim) || kv_heads <= 0 || kv_heads > 1024 || (Q && (q_heads <= 0 || q_heads > 65536))) return ITQ3S_ERR_SHAPE;
+    if (T <= 0 || T > kMostAppended || !head_dim_ok(head_dim) || kv_heads <= 0 || kv_heads > 1024 || (Q && (q_heads <= 0 || q_heads > 65536))) return ITQ3S_ERR_SHAPE;
     if (rot < 0 || rot > head_dim || rot % 16 != 0) return ITQ3S_ERR_SHAPE;
     if (!(eps >= 0.f) || !isfinite(eps) || !isfinite(gain)) return ITQ3S_ERR_SHAPE;
     if ((in_dtype != ITQ3S_F32 && in_dtype != ITQ3S_F16) || (out_dtype != ITQ3S_F32 && out_dtype != ITQ3S_F16)) return ITQ3S_ERR_DTYPE;
@@ -99,7 +100,7 @@ int itq3s_cache_read(const itq3s_cache* cache, const int64_t* slots, int64_t T, 
     if (!cache || !slots || !K_out || !V_out) return ITQ3S_ERR_NULL;
     int rc = cache_ok(cache);
     if (rc != 0) return rc;
-    if (T <= 0 || T > 0x7fffffffLL) return ITQ3S_ERR_SHAPE;
+    if (T <= 0 || T > kMostRead) return ITQ3S_ERR_SHAPE;
     if (out_dtype != ITQ3S_F32 && out_dtype != ITQ3S_F16) return ITQ3S_ERR_DTYPE;
     const size_t out = out_dtype == ITQ3S_F16 ? 2 : 4;
     if ((rc = rows_ok(K_out, ldk, cache->kv_heads, cache->head_dim, out)) != 0 || (rc = rows_ok(V_out, ldv, cache->kv_heads, cache->head_dim, out)) != 0) return rc;
@@ -108,7 +109,7 @@ int itq3s_cache_read(const itq3s_cache* cache, const int64_t* slots, int64_t T, 
 }
 
 size_t itq3s_cache_attention_workspace_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
-    if (T <= 0 || seqs <= 0 || seqs > kMostSeqs || !heads_ok(q_heads, kv_heads) || T > kMostRows / (q_heads / kv_heads) || !head_dim_ok(head_dim) || max_q <= 0 || max_kv <= 0 ||
+    if (T <= 0 || !heads_ok(q_heads, kv_heads) || seqs <= 0 || seqs > itq3s::kMostUnits / kv_heads || T > kMostRows / (q_heads / kv_heads) || !head_dim_ok(head_dim) || max_q <= 0 || max_kv <= 0 ||
         max_kv > kMostRows)
         return 256;
     return itq3s::cache_attention_bytes(T, seqs, q_heads, kv_heads, head_dim, max_q < T ? max_q : T, max_kv);
@@ -120,7 +121,9 @@ int itq3s_cache_attention(const void* Q, int64_t ldq, int64_t T, int q_heads, co
     if (!Q || !cache || !q_starts || !kv_lens || !pages || !out) return ITQ3S_ERR_NULL;
     int rc = cache_ok(cache);
     if (rc != 0) return rc;
-    if (!heads_ok(q_heads, cache->kv_heads) || T <= 0 || seqs <= 0 || seqs > kMostSeqs || T > kMostRows / (q_heads / cache->kv_heads)) return ITQ3S_ERR_SHAPE;
+    if (!heads_ok(q_heads, cache->kv_heads) || T <= 0 || seqs <= 0 || seqs > itq3s::kMostUnits / cache->kv_heads ||
+        T > kMostRows / (q_heads / cache->kv_heads))
+        return ITQ3S_ERR_SHAPE;
     if (ld_pages <= 0 || ld_pages > kMostRows / cache->page_tokens || max_q <= 0 || max_kv <= 0 || max_kv > kMostRows || !(fabsf(scale) <= kMostScale)) return ITQ3S_ERR_SHAPE;
     if ((rc = rows_ok(Q, ldq, q_heads, cache->head_dim, 2)) != 0 || (rc = rows_ok(out, ldo, q_heads, cache->head_dim, 2)) != 0) return rc;
     if (!aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(pages, 4) || (status_flags && !aligned(status_flags, 4))) return ITQ3S_ERR_ALIGN;
@@ -135,7 +138,8 @@ int itq3s_cache_attention(const void* Q, int64_t ldq, int64_t T, int q_heads, co
 int itq3s_prompt_attention(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T, int q_heads, int kv_heads, int head_dim,
                            const int32_t* starts, int64_t seqs, int64_t max_len, int causal, float scale, void* out, int64_t ldo, void* stream) {
     if (!Q || !K || !V || !starts || !out) return ITQ3S_ERR_NULL;
-    if (!heads_ok(q_heads, kv_heads) || !head_dim_ok(head_dim) || T <= 0 || T > kMostRows / (q_heads / kv_heads) || seqs <= 0 || seqs > kMostSeqs || max_len <= 0 || !(fabsf(scale) <= kMostScale))
+    if (!heads_ok(q_heads, kv_heads) || !head_dim_ok(head_dim) || T <= 0 || T > kMostRows / (q_heads / kv_heads) || seqs <= 0 || seqs > itq3s::kMostUnits / kv_heads ||
+        max_len <= 0 || !(fabsf(scale) <= kMostScale))
         return ITQ3S_ERR_SHAPE;
     int rc = 0;
     if ((rc = rows_ok(Q, ldq, q_heads, head_dim, 2)) != 0 || (rc = rows_ok(K, ldk, kv_heads, head_dim, 2)) != 0 || (rc = rows_ok(V, ldv, kv_heads, head_dim, 2)) != 0 ||

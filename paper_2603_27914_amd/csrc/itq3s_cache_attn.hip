@@ -707,7 +707,7 @@ Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_
     const int64_t blocks = (max_kv + kCacheBlock - 1) / kCacheBlock;
     p.share = rows > 128 ? Share::none : rows > 16 ? Share::tiles : Share::blocks;
     const int64_t per = p.share == Share::none ? (head_dim < 256 ? 128 : 64) : p.share == Share::tiles ? 64 : 16;
-    p.tiles = (rows + per - 1) / per;
+    p.tiles = most_tiles((rows + per - 1) / per, units);
     // Few and short sequences: sixteen wavefronts share one, and no second launch joins parts.
     p.wide = p.share == Share::blocks && head_dim <= 128 && blocks <= 64 && units <= cus;
     // Else as many parts as give every unit two workgroups. Four a unit, which also fit where a workgroup has four wavefronts,
@@ -738,11 +738,16 @@ int start(const AttnArgs& a, int64_t grid, hipStream_t st) {
 
 template <int D>
 int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStream_t st) {
-    int rc;
+    int rc = 0;
     if (p.share == Share::none) rc = start<D, D == 256 ? 1 : 2, 4, Share::none, 1>(a, grid, st);
     else if (p.share == Share::tiles) rc = start<D, 1, 8, Share::tiles, 2>(a, grid, st);
-    else if (p.wide) rc = start<D, 1, D <= 128 ? 16 : 4, Share::blocks, D <= 128 ? 1 : 2>(a, grid, st);
-    else rc = start<D, 1, 4, Share::blocks, 2>(a, grid, st);
+    else {
+        bool wide = false;
+        if constexpr (D <= 128) wide = p.wide;
+        if (!wide) rc = start<D, 1, 4, Share::blocks, 2>(a, grid, st);
+        if constexpr (D <= 128)
+            if (wide) rc = start<D, 1, 16, Share::blocks, 1>(a, grid, st);
+    }
     if (rc != 0 || p.splits <= 1) return rc;
     int groups = 1;
     while (2 * groups <= p.splits && groups < 2048 / D) groups *= 2;
@@ -770,10 +775,9 @@ int launch_cache_attention(const CacheAttentionCall& c, hipStream_t st) {
     a.scale = (float)((double)c.scale * 1.44269504088896340736 / (D == 64 ? 8.0 : D == 128 ? 11.313708498984760390 : 16.0));
     if (__builtin_fabsf(a.scale) < 1e-30f) a.scale = 0.f;  // no score leaves 2^-40 then: all weights alike
     a.q_heads = c.q_heads, a.kv_heads = c.cache.kv_heads, a.group = G, a.seqs = (int)c.seqs, a.tiles = (int)p.tiles, a.splits = p.splits, a.split_blocks = p.split_blocks;
-    a.page_units = c.cache.kv_heads * c.cache.page_blocks * (32 * D + 128) / 128;
+    a.page_units = c.cache.kv_heads * c.cache.page_blocks * (D / 4 + 1);  // of 128 bytes: at most 2^21 * 65
     a.page_shift = __builtin_ctz((unsigned)c.cache.page_blocks);
     const int64_t grid = c.seqs * c.cache.kv_heads * p.tiles * p.splits;
-    if (grid > 0x7fffffffLL) return -2;
     if (D == 64) return start<64>(a, p, grid, c.max_q, st);
     if (D == 128) return start<128>(a, p, grid, c.max_q, st);
     return start<256>(a, p, grid, c.max_q, st);

@@ -197,8 +197,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 
 template <int D, int kWaves>
 int start(PromptArgs a, int64_t max_len, hipStream_t st) {
-    const int64_t tiles = (max_len * a.group + 32 * kWaves - 1) / (32 * kWaves), grid = tiles * a.seqs * a.kv_heads;
-    if (grid > 0x7fffffffLL) return -2;
+    const int64_t units = (int64_t)a.seqs * a.kv_heads, tiles = most_tiles((max_len * a.group + 32 * kWaves - 1) / (32 * kWaves), units), grid = tiles * units;
     a.tiles = (int)tiles;
     prompt_kernel<D, kWaves><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, st>>>(a);
     return hipGetLastError() == hipSuccess ? 0 : -6;

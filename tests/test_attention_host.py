@@ -157,6 +157,16 @@ def test_prompt_attention_refuses(L, memory):
         assert c(**other) == -3, other
 
 
+def test_sizes_beyond_a_launch_are_refused(L, memory):
+    """A launch has less than 2^32 threads."""
+    _, ok, _, _ = memory
+    wide = desc(ok, kv_heads=1024)
+    assert L.itq3s_cache_append(None, 0, 0, ok, 128, ok, 128, 2**24 + 1, 1, 2, 64, None, None, 0.0, None, None, 0, 0, 1.0, None, 0, None, 0, 1, desc(ok), ok, None, None) == -2
+    assert L.itq3s_cache_read(desc(ok), ok, 2**28 + 1, ok, 128, ok, 128, 0, None, None) == -2
+    assert L.itq3s_cache_attention(ok, 65536, 1, 1024, wide, ok, ok, 4097, ok, 1, 1, 32, 0.1, ok, 65536, ok, 4096, None, None) == -2
+    assert L.itq3s_prompt_attention(ok, 65536, ok, 65536, ok, 65536, 1, 1024, 1024, 64, ok, 4097, 1, 1, 0.1, ok, 65536, None) == -2
+
+
 def test_binding_refuses_what_the_library_cannot_see(monkeypatch):
     """Pointers carry neither sizes nor types: those are checked before the call (here on CPU tensors that pass for device ones, with a library that is
     not to be reached)."""
@@ -221,3 +231,10 @@ def test_attention_kernels_keep_their_registers(source):
     asm = subprocess.run(["hipcc", *build.flags(src), "--cuda-device-only", "-S", src, "-o", "-"], check=True, stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True).stdout
     kernels = re.findall(r"\.amdhsa_kernel (\S+).*?\.amdhsa_private_segment_fixed_size (\d+)", asm, flags=re.S)
     assert kernels and [k for k in kernels if k[1] != "0"] == []
+    # the copies written in assembly set m0, which cannot be named as clobbered: where there are any, nothing else uses it
+    written, other = [], []
+    for block in re.split(r"(;;?#ASMSTART.*?;;?#ASMEND)", asm, flags=re.S):
+        (written if block.lstrip(";").startswith("#ASMSTART") else other).append(block)
+    copies = [w for w in written if re.search(r"\bm0\b", w)]
+    assert bool(copies) == (source == "prompt")
+    assert not copies or not any(re.search(r"^\s+\w.*\bm0\b", o, flags=re.M) for o in other)

@@ -480,6 +480,74 @@ def test_prompts_do_not_see_each_other(gpu):
     assert torch.equal(a[:40], b[:40]) and torch.equal(a[97:], b[97:]) and bool(torch.isnan(b[40:97]).all())
 
 
+# ---- sizes at their ends
+
+
+def test_pages_of_more_than_two_gib(gpu):
+    """One page of 65536 tokens of 128 heads of 256 is 2.2e9 bytes: the second page against the same rows in small pages."""
+    torch, binding = gpu
+    rng = np.random.default_rng(21)
+    T, H, D, page = 70, 128, 256, 65536
+    k, v, q = (dev(torch, rows(rng, T, H, D, "f16")) for _ in range(3))
+    small, large = binding.alloc_cache(2, 64, H, D), binding.alloc_cache(2, page, H, D)
+    assert large.data.numel() > 2**32
+    here = dev(torch, np.arange(T, dtype=np.int64))
+    binding.itq3s_cache_append(None, k, v, None, None, small, here)
+    flags = flag(torch)
+    for at in (page, 2 * page - T):
+        binding.itq3s_cache_append(None, k, v, None, None, large, here + at, status_flags=flags)
+        for a, b in zip(binding.itq3s_cache_read(small, here), binding.itq3s_cache_read(large, here + at, status_flags=flags)):
+            assert torch.equal(a, b)
+    starts, lens = dev(torch, np.array([0, 1], dtype=np.int32)), dev(torch, np.array([T], dtype=np.int32))
+    for n in (1, 3, T):  # rows alone, in shared tiles, and in tiles of their own
+        starts[1] = n
+        a = binding.itq3s_cache_attention(q[:n], small, starts, lens, dev(torch, np.array([[0, 1]], dtype=np.int32)), max_kv=T)
+        b = binding.itq3s_cache_attention(q[:n], large, starts, lens, dev(torch, np.array([[1]], dtype=np.int32)), max_kv=T, status_flags=flags)
+        assert torch.equal(a, b)
+    assert int(flags.item()) == 0
+
+
+def test_many_sequences_and_estimates_far_too_high(gpu):
+    """Rows of two sequences among 2^15 of none, and as many rows expected of each as there are in all: tiles by the million."""
+    torch, binding = gpu
+    rng = np.random.default_rng(22)
+    S, T, D, Hq, H, page = 2**15, 512, 64, 128, 8, 32
+    q, k, v = dev(torch, rows(rng, T, Hq, D, "f16")), dev(torch, rows(rng, T, H, D, "f16")), dev(torch, rows(rng, T, H, D, "f16"))
+    few = np.array([0, 500, T], dtype=np.int32)
+    many = np.zeros(S + 1, dtype=np.int32)
+    many[8:], many[30000:] = 500, T
+    few, many = dev(torch, few), dev(torch, many)
+    assert torch.equal(binding.itq3s_prompt_attention(q, k, v, D, few), binding.itq3s_prompt_attention(q, k, v, D, many))
+    cache = binding.alloc_cache(17, page, H, D)
+    slots = np.concatenate([np.arange(500), 512 + np.arange(12)])
+    binding.itq3s_cache_append(None, k, v, None, None, cache, dev(torch, slots))
+    table, lens = np.zeros((2, 16), dtype=np.int32), np.array([500, 12], dtype=np.int32)
+    table[0], table[1, 0] = np.arange(16), 16
+    all_tables, all_lens = np.zeros((S, 16), dtype=np.int32), np.zeros(S, dtype=np.int32)
+    all_tables[7], all_tables[29999], all_lens[7], all_lens[29999] = table[0], table[1], 500, 12
+    a = binding.itq3s_cache_attention(q, cache, few, dev(torch, lens), dev(torch, table), max_kv=512)
+    b = binding.itq3s_cache_attention(q, cache, many, dev(torch, all_lens), dev(torch, all_tables), max_kv=512)
+    assert torch.equal(a, b)
+
+
+def test_read_of_rows_far_apart_with_others_that_are_not_there(gpu):
+    """Every listed row in another block, and among them padding and slots behind the cache."""
+    torch, binding = gpu
+    rng = np.random.default_rng(23)
+    H, D, page, pages = 2, 128, 32, 40
+    k, v = (dev(torch, rows(rng, page * pages, H, D, "f16")) for _ in range(2))
+    cache = binding.alloc_cache(pages, page, H, D)
+    binding.itq3s_cache_append(None, k, v, None, None, cache, dev(torch, np.arange(page * pages, dtype=np.int64)))
+    K, V = binding.itq3s_cache_read(cache, dev(torch, np.arange(page * pages, dtype=np.int64)))  # (neighbours)
+    slots = np.concatenate([rng.permutation(pages) * page + rng.integers(0, page, pages) for _ in range(3)])
+    slots[rng.permutation(len(slots))[:50]] = rng.choice([-1, -(2**62), page * pages, 2**62], 50)
+    slots[:32] = np.where(np.arange(32) % 3 == 0, slots[:32], -1)
+    live = dev(torch, (slots >= 0) & (slots < page * pages))
+    at = dev(torch, slots.clip(0, page * pages - 1))
+    for got, all_rows in zip(binding.itq3s_cache_read(cache, dev(torch, slots)), (K, V)):
+        assert torch.equal(got, torch.where(live[:, None], all_rows[at], torch.zeros_like(got)))
+
+
 # ---- together
 
 
