@@ -12,8 +12,7 @@
 //
 // A lane holds eight channels of a row: 8, 16 or 32 lanes a row, 8, 4 or 2 rows a wavefront.  The rows of one wavefront are heads of
 // one token (a kilobyte of neighbouring memory an instruction; they share the sines, so each row of lanes works out its
-// part of them) or, for values where there are many tokens, neighbouring tokens (so that their bytes share words of
-// memory).  A wavefront walks over heads with the sines that it has worked out once.
+// part of them) or, for values, neighbouring tokens (so that their bytes share words of memory).  A wavefront walks over heads with the sines that it has worked out once.
 #include <type_traits>
 
 #include "itq3s_attention.h"
@@ -84,9 +83,8 @@ struct AppendArgs {
     int q_heads, kv_heads, rot, interleaved;
     float eps, gain;
     int page_blocks;                  // blocks of 32 tokens a page
-    int tokens;                       // of values: neighbouring tokens in a wavefront (1 or as many as it has rows)
     int q_step, k_step, v_step;       // heads that a wavefront walks over
-    int64_t groups;                   // groups of tokens for values (else every token is one)
+    int64_t groups;                   // of neighbouring tokens, whose values a wavefront takes
     int64_t k_jobs, v_jobs, q_jobs;   // wavefronts
     int few_are_kv, few_blocks, period;  // workgroups of keys and values (or of queries), one among so many while there are any
 };
@@ -260,12 +258,12 @@ __device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8]
     if (live && ch == 0) *reinterpret_cast<_Float16*>(base + 32 * D + 4 * t + (is_value ? 2 : 0)) = s;
 }
 
-// One wavefront: its token group's rows for heads h0 .. h1 - 1 of the queries (what 0), the keys (1) or the values (2).
+// One wavefront: its token's rows (of values: its tokens') for heads h0 .. h1 - 1 of the queries (what 0), the keys (1) or the values (2).
 template <int D, typename In, typename Out, int kWhat>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int64_t group, int h0, int h1) {
     typedef typename std::conditional<kWhat == 0, float, double>::type R;
     const int row = Rows<D>::row(), ch = Rows<D>::channel();
-    const bool by_token = kWhat == 2 && a.tokens > 1;
+    constexpr bool by_token = kWhat == 2;
     const int64_t token = by_token ? group * Rows<D>::kRows + row : group;
     const bool here = token < a.T;
     const int64_t tok = here ? token : a.T - 1;
@@ -512,16 +510,17 @@ int launch_append(const AppendCall& c, hipStream_t st) {
     a.q_heads = c.Q != nullptr ? c.q_heads : 0, a.kv_heads = c.kv_heads, a.rot = c.rot, a.interleaved = c.interleaved, a.eps = c.eps, a.gain = c.gain;
     a.data = c.cache.data, a.page_blocks = c.cache.data != nullptr ? c.cache.page_blocks : 1;
     a.slots_end = c.cache.data != nullptr ? c.cache.pages * c.cache.page_blocks * kCacheBlock : 0;
-    // Values: neighbouring tokens in a wavefront where that leaves every compute unit four of them.
-    a.tokens = c.T * c.kv_heads / rows >= 4 * (int64_t)cu_count() ? rows : 1;
-    a.groups = (c.T + a.tokens - 1) / a.tokens;
-    // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  16 a unit are plenty, and 32
+    // Values: neighbouring tokens in a wavefront.  (Heads of one token as for keys are no better for one token, and worse for many: 10000
+    // tokens, 32 heads of 128 203 us instead of 198.)
+    a.groups = (c.T + rows - 1) / rows;
+    // Heads that a wavefront walks over: more of them share the sines, fewer make more wavefronts.  8 a unit are plenty (us with 4, 8 and
+    // 16, 64 and 8 heads of 128: 500 tokens 15.5, 17.1 and 18.2, 1000 22.0, 20.1 and 22.1, 2000 40.8, 30.3 and 29.6), and 32
     // of the short ones of values (11385 tokens, 64 and 8 heads of 128: 8, 4, 2 and 1 heads 116, 114, 106 and 118 us).
     auto heads_of = [&](int heads, int step, int64_t groups, int plenty) {
         while (step < heads && groups * ((heads + 2 * step - 1) / (2 * step)) >= plenty * (int64_t)cu_count()) step *= 2;
         return step;
     };
-    a.q_step = heads_of(a.q_heads, rows, c.T, 16), a.k_step = heads_of(c.kv_heads, rows, c.T, 16), a.v_step = heads_of(c.kv_heads, a.tokens > 1 ? 1 : rows, a.groups, 32);
+    a.q_step = heads_of(a.q_heads, rows, c.T, 8), a.k_step = heads_of(c.kv_heads, rows, c.T, 8), a.v_step = heads_of(c.kv_heads, 1, a.groups, 32);
     a.k_jobs = c.K != nullptr ? c.T * ((c.kv_heads + a.k_step - 1) / a.k_step) : 0;
     a.v_jobs = c.V != nullptr ? a.groups * ((c.kv_heads + a.v_step - 1) / a.v_step) : 0;
     a.q_jobs = a.q_heads > 0 ? c.T * ((a.q_heads + a.q_step - 1) / a.q_step) : 0;

@@ -378,7 +378,7 @@ __device__ __forceinline__ void turn_back(floatx4 (&o)[D / 16][CT], int ct, int 
 // How the wavefronts of a workgroup share its rows and blocks.
 enum class Share {
     blocks,  // 16 rows, all take blocks in turn
-    tiles,   // 16, 32 or 64 rows, as many as the sequence has: wavefronts of different rows take the same blocks at one time
+    tiles,   // 16 or 32 rows (64 if it has more than was said), as many as the sequence has: wavefronts of different rows take the same blocks at one time
     none     // 16 CT rows of its own a wavefront, every block
 };
 
@@ -701,21 +701,36 @@ struct Plan {
     int64_t tiles;
     int splits, split_blocks;
 };
-Plan plan_of(int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
+Plan plan_of(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
     Plan p;
-    const int64_t rows = max_q * (q_heads / kv_heads), units = seqs * kv_heads, cus = cu_count();
+    const int64_t group = q_heads / kv_heads, rows = max_q * group, all_rows = T * group, units = seqs * kv_heads, cus = cu_count();
     const int64_t blocks = (max_kv + kCacheBlock - 1) / kCacheBlock;
-    p.share = rows > 128 ? Share::none : rows > 16 ? Share::tiles : Share::blocks;
-    const int64_t per = p.share == Share::none ? (head_dim < 256 ? 128 : 64) : p.share == Share::tiles ? 64 : 16;
+    // Rows of its own a wavefront: unpacks a block once for 32 rows and loads it four times as often as wavefronts that share it,
+    // so it takes many rows -- of a sequence to fill a workgroup, and of all to fill the card -- or much to do for each.  us
+    // with own rows and with shared blocks, 64 query and 8 kv heads of 128: 128 rows of 4000 tokens 58 and 46, 256 77 and 73, 512
+    // 113 and 126; 128 rows of 16500 120 and 137, of 1000 37 and 25; 16 sequences of 2000 with 16 rows 56 and 57.
+    const int64_t own = head_dim < 256 ? 128 : 64, most_rows = all_rows < rows * seqs ? all_rows : rows * seqs;
+    const bool many = rows >= own && 2 * all_rows >= own * seqs && (most_rows * kv_heads >= 64 * cus || most_rows * kv_heads >= 8192 * cus / blocks);
+    // Two tiles of 16 rows in one workgroup of eight wavefronts, or in two of four: us of ragged batches of up to 4 rows, 61 of up to 8000
+    // tokens 81 and 102, 60 of 4000 50 and 56, 20 of 8000 43 and 52; of equal ones, 16 of 4000 39 and 32.  For more tiles: 60
+    // of up to 9 rows 110 and 77, of 5 rows 79 and 60.
+    p.share = many ? Share::none : rows > 16 && rows <= 32 ? Share::tiles : Share::blocks;
+    const int64_t per = p.share == Share::none ? own : p.share == Share::tiles ? 32 : 16;
     p.tiles = most_tiles((rows + per - 1) / per, units);
-    // Few and short sequences: sixteen wavefronts share one, and no second launch joins parts.
-    p.wide = p.share == Share::blocks && head_dim <= 128 && blocks <= 64 && units <= cus;
-    // Else as many parts as give every unit two workgroups. Four a unit, which also fit where a workgroup has four wavefronts,
-    // measured for 8 heads of 128: one sequence of 131072 tokens 41.9 us, with two 40.7; 64 of 1000 23.9 and 18.9; one of
-    // 16000 20.7 and 16.2; and 16 of 2500 with 32 heads 40.2 and 36.7. One a unit: 131072 tokens 45.8 us.
-    const int64_t places = 2 * cus, work = units * p.tiles * blocks;
+    // Sixteen wavefronts share one short sequence, and no second launch joins parts.  us with them and with parts of four: one
+    // sequence, 8 kv heads, of 120 tokens 8.7 and 8.2, 250 9.3 and 10.8, 1000 11.6 and 12.2, 2000 14.5 and 12.5; 8 of 2000
+    // 14.7 and 15.8, of 4000 20.5 and 18.1; 32 of 6000 47 and 52; 48 of 250 16.3 and 16.2, of 120 15.1 and 9.9.
+    p.wide = p.share == Share::blocks && rows <= 16 && head_dim <= 128 && blocks > 4 && units <= cus && blocks <= 32 + units * 256 / cus;
+    // Else as many parts as give every unit two workgroups (three of Share::tiles, for their ragged batches: above 81, with two 89).
+    // Four a unit, which also fit where a workgroup has four wavefronts, measured for 8 kv heads of 128: one sequence of
+    // 131072 tokens 41.9 us, with two 40.7; 64 of 1000 23.9 and 18.9; one of 16000 20.7 and 16.2; 16 of 2500 with 32 heads
+    // 40.2 and 36.7.  One a unit: 131072 tokens 45.8 us.  (Sequences have rows for so many tiles at most.)
+    const int64_t all_tiles = kv_heads * (all_rows / per + seqs), some_tiles = units * p.tiles;
+    const int64_t places = (p.share == Share::tiles ? 3 : 2) * cus, work = (all_tiles < some_tiles ? all_tiles : some_tiles) * blocks;
     int64_t per_split = p.wide ? blocks : (work + places - 1) / places;
-    const int64_t few = p.share == Share::none ? 16 : 4;
+    // Parts of own rows cost the most to join: 512 rows of 1000 tokens in parts of 16 blocks 54 us, of 32 (one part) 46, 200 rows of
+    // 4000 83 and 72.  Shared ones: one row of 4000 tokens in parts of 2, 4 and 8 blocks 14.8, 13.1 and 13.2.
+    const int64_t few = p.share == Share::none ? 32 : 4;
     if (per_split < few) per_split = few;
     const int64_t least = (blocks + kMaxSplits - 1) / kMaxSplits;
     if (per_split < least) per_split = least;
@@ -759,14 +774,14 @@ int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStre
 }  // namespace
 
 size_t cache_attention_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv) {
-    const Plan p = plan_of(seqs, q_heads, kv_heads, head_dim, max_q, max_kv);
+    const Plan p = plan_of(T, seqs, q_heads, kv_heads, head_dim, max_q, max_kv);
     if (p.splits <= 1) return 256;
     return (size_t)p.splits * (size_t)T * (size_t)q_heads * (size_t)(head_dim + 2) * 4 + 256;
 }
 
 int launch_cache_attention(const CacheAttentionCall& c, hipStream_t st) {
     const int G = c.q_heads / c.cache.kv_heads, D = c.cache.head_dim;
-    const Plan p = plan_of(c.seqs, c.q_heads, c.cache.kv_heads, D, c.max_q, c.max_kv);
+    const Plan p = plan_of(c.T, c.seqs, c.q_heads, c.cache.kv_heads, D, c.max_q, c.max_kv);
     AttnArgs a{};
     a.Q = c.Q, a.starts = c.starts, a.kv_lens = c.kv_lens, a.pages = c.pages, a.data = c.cache.data, a.out = c.out, a.flags = c.flags;
     a.part = static_cast<float*>(c.workspace);
