@@ -509,8 +509,11 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
                 load_keys<D>(next.at, r.k, lane);
                 __builtin_amdgcn_sched_barrier(0);
                 half8 p[CT];
+                // (ahead of others' products: the vector ALU is what a unit has least of.  A chunk of 512 rows of 16500 tokens 365 -> 356 us)
+                __builtin_amdgcn_s_setprio(1);
                 weights<D, CT, kParts>(s, r.s, now.base, q, see, see_all, sq.len, st, p, g);
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
                 load_steps<D>(next.at, r.s, lane);
                 __builtin_amdgcn_sched_barrier(0);
                 products<D, CT>(r.v, p, st);
