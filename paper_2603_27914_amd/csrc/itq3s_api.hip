@@ -405,10 +405,10 @@ const char* itq3s_strerror(int status) {
     switch (status) {
         case ITQ3S_OK: return "ok";
         case ITQ3S_ERR_NULL: return "a required pointer is NULL";
-        case ITQ3S_ERR_SHAPE: return "bad shape: sizes must be positive, K a multiple of 256, leading dimensions large enough";
+        case ITQ3S_ERR_SHAPE: return "bad shape: sizes must be positive and within the call's limits, K a multiple of 256, head_dim 64, 128 or 256, leading dimensions large enough";
         case ITQ3S_ERR_ALIGN: return "pointer or leading dimension not aligned as required";
         case ITQ3S_ERR_DTYPE: return "dtype must be ITQ3S_F32 or ITQ3S_F16";
-        case ITQ3S_ERR_WORKSPACE: return "workspace missing or smaller than itq3s_matmul_workspace_bytes()";
+        case ITQ3S_ERR_WORKSPACE: return "workspace missing or smaller than itq3s_matmul_workspace_bytes() (itq3s_cache_attention_workspace_bytes())";
         case ITQ3S_ERR_LAUNCH: return "HIP refused the kernel launch";
     }
     return "unknown status";

@@ -13,6 +13,14 @@
 //
 // Few rows: the wavefronts of a workgroup take blocks in turn and meet in LDS.  Many rows: each has its own rows.  A
 // long context is split over workgroups besides; combine_kernel joins the parts.
+//
+// What bounds it.  Few rows: the stream of blocks -- 16 sequences of 1500 to 2500 tokens, 32 heads of 128 with one row each, 138 MB, in
+// 30 us, 4.6 TB/s (a copy: 5.2); one of 131072 tokens, 8 kv heads, in 25 us and 5 for the join.  A wavefront waits for memory
+// for 40 % of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four or eight a SIMD),
+// or two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
+// 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (63 and 33 %
+// of it): 512 rows of 64 heads over 16500 tokens 355 us, 770 TFLOP/s.  Unpacking once for four wavefronts into LDS saves a
+// third of the vector instructions and took 340 to 385 us: it leaves room for no more wavefronts, and they wait for each other.
 #include "itq3s_attention.h"
 #include "itq3s_cache.h"
 
@@ -625,7 +633,8 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
 }
 
 // Joins the parts of rows whose sequence was split: D / 8 lanes a part, `lanes` groups of them a row (a power of two up to a
-// workgroup's), the groups of a row beside each other.
+// workgroup's), the groups of a row beside each other.  64 rows of 64 parts 5 us, of which a launch is half; 32768 rows of two, 34 MB,
+// 13 us.
 template <int D>
 __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a, int groups_of_row) {
     constexpr int kLanes = D / 8, kGroups = 256 / kLanes;

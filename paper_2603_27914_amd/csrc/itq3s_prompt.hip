@@ -11,8 +11,9 @@
 // row against bank conflicts (by the address that each lane copies from); V^T is read with the transposing LDS read.
 // Three workgroups of four wavefronts a compute unit: nothing in a wavefront overlaps its products with its exponentials, the
 // others do.  (One wavefront a SIMD with 64 rows, which reads LDS half as often, and its two halves interleaved by hand: 606
-// us where this takes 546, 8192 tokens, 32 query and 8 kv heads of 128.)  There the matrix pipes are busy for 58 % of the
-// time, the vector ALU for 53 %, and the clock is down to 1.66 GHz by what that draws.
+// us where this takes 546, 8192 tokens, 32 query and 8 kv heads of 128.)  That is 1.03 PFLOP/s, where a matrix product of
+// 8192 x 8192 x 8192 reaches 1.21; the matrix pipes are busy for 58 % of the time, the vector ALU for 46 to 53 %, and the clock is down
+// to 1.66 GHz by what that draws.  Neither products nor softmax first (wavefront priorities) helps: 556 and 562 us.
 #include "itq3s_attention.h"
 #include "itq3s_cache.h"
 
@@ -204,9 +205,12 @@ int start(PromptArgs a, int64_t max_len, hipStream_t st) {
 }
 template <int D>
 int start(const PromptArgs& a, int64_t max_len, hipStream_t st) {
-    // four wavefronts share a tile, or two where four would leave compute units without a workgroup
-    const bool few = (max_len * a.group + 127) / 128 * a.seqs * a.kv_heads < cu_count();
-    return few ? start<D, 2>(a, max_len, st) : start<D, 4>(a, max_len, st);
+    // Four wavefronts share a tile, or two where four would leave compute units without a workgroup: us with two and with four, 32 query
+    // and 8 kv heads of 128, one sequence of 250 tokens 11.1 and 12.0, of 1000 (the border) 29.0 and 30.0, of 2000 57.3 and 53.6,
+    // 7 of 700 57.5 and 50.8; 16 and 8 heads of 256, 1000 tokens 47.7 and 50.0, 7 of 700 73.8 and 52.3.  (There are rows for so many
+    // tiles at most, whatever max_len says.)
+    const int64_t tiles = (max_len * a.group + 127) / 128 * a.seqs, all = (int64_t)a.T * a.group / 128 + a.seqs;
+    return (tiles < all ? tiles : all) * a.kv_heads < cu_count() ? start<D, 2>(a, max_len, st) : start<D, 4>(a, max_len, st);
 }
 
 }  // namespace
