@@ -9,13 +9,14 @@
 //   O^T += C_v^T P'^T   with P' = exp2(y - m) s_v: the accumulator layout of S^T is the operand layout of P'^T
 // Online softmax in base 2.  Steps of values go into P' and may be any fp16, so the reference m follows the largest
 // y + exponent(s_v): P' stays within fp16 whatever the steps are, and l = sum exp2(y - m) in fp32 has the range to follow.
-// m only moves when a row's weights would pass 2^8 (then O and l are scaled): a block costs no rescaling otherwise.
+// m only moves when a row's weights would pass 2^15 (then O and l are scaled, weights up to 2^7 again): a block costs no rescaling
+// otherwise, and weights keep all of fp16's bits down to 2^-21 of a long row's largest.
 //
 // Few rows: the wavefronts of a workgroup take blocks in turn and meet in LDS.  Many rows: each has its own rows.  A
 // long context is split over workgroups besides; combine_kernel joins the parts.
 //
 // What bounds it.  Few rows: the stream of blocks -- 16 sequences of 1500 to 2500 tokens, 32 heads of 128 with one row each, 138 MB, in
-// 30 us, 4.6 TB/s (a copy: 5.2); one of 131072 tokens, 8 kv heads, in 25 us and 5 for the join.  A wavefront waits for memory
+// 31 us, 4.5 TB/s (a copy: 5.2); one of 131072 tokens, 8 kv heads, in 25 us and 5 for the join.  A wavefront waits for memory
 // for 40 % of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four or eight a SIMD),
 // or two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
 // 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (63 and 33 %
@@ -29,8 +30,8 @@ namespace itq3s {
 namespace {
 
 constexpr float kNoRow = -1e30f;    // reference of a row that has seen nothing
-constexpr float kHeadroom = 8.f;    // weights may reach 2^8 before the reference moves
-constexpr int kExpBias = 14;        // s < 2^(E - 14) for an fp16 with exponent field E
+constexpr float kHeadroom = 8.f;    // weights may grow by 2^8 before the reference moves
+constexpr int kExpBias = 21;        // s < 2^(E - 14) for an fp16 with exponent field E; weights take 2^7 of what fp16 has above 2^8
 constexpr int kMaxSplits = 256;
 
 struct AttnArgs {
@@ -181,7 +182,8 @@ struct Mantissas {
 __device__ __forceinline__ half8 key_operand(uint32_t w, const Mantissas& m) {
     return as_halves((w & 0x000f000fu) | m.low, (w & 0x00f000f0u) | m.high, ((w >> 8) & 0x000f000fu) | m.low, ((w >> 8) & 0x00f000f0u) | m.high);
 }
-// Stored digits of values, as subnormal fp16: n 2^-24, or n 2^-20 for the upper nibbles, exactly what the matrix cores take them for.
+// Stored digits of values, as subnormal fp16: n 2^-24, or n 2^-20 for the upper nibbles, exactly what the matrix cores take them for
+// (and 8 less, where few rows share blocks).
 __device__ __forceinline__ half8 value_operand_low(uint32_t u, uint32_t w) { return as_halves(u & 0x000f000fu, (u >> 8) & 0x000f000fu, w & 0x000f000fu, (w >> 8) & 0x000f000fu); }
 __device__ __forceinline__ half8 value_operand_high(uint32_t u, uint32_t w) { return as_halves(u & 0x00f000f0u, (u >> 8) & 0x00f000f0u, w & 0x00f000f0u, (w >> 8) & 0x00f000f0u); }
 
@@ -238,8 +240,12 @@ __device__ __forceinline__ void load_queries(const unsigned char* lds, uint32_t 
     q.unit[ct] = *reinterpret_cast<const float*>(lds + row + kParts * 2 * D + 4);
 }
 
-// O^T in the units of value_operand: accumulators of even channel tiles times 2^24, of odd ones 2^20, less `eight` (of sum 8 P',
-// in the even ones' units) each.
+// O^T in the units of value_operand: accumulators of even channel tiles times 2^24, of odd ones 2^20.  With digits n = c + 8 each has
+// `eight` too much (of sum 8 P', in the even ones' units); the matrix cores cut the sum of a product's terms, which over a long context adds
+// up against that sum: a row of 131072 tokens comes out 6e-4 off.  So few rows, whose time is the memory's, take 8 off the digits
+// (kCentred: 3.3e-4, and 1 to 2 % of time), and many rows, whose time is the vector ALU's, do not (16500 tokens 4.5e-4, where
+// it were 4.1e-4 and 4 to 12 % of time; 2.1e-4 of each is the result's rounding to fp16).  Nor do sixteen wavefronts of a
+// short sequence (2.9e-4 either way).
 template <int D, int CT>
 struct State {
     floatx4 o[D / 16][CT], eight[CT];
@@ -270,7 +276,7 @@ __device__ __forceinline__ void scores(const uint32_t (&k)[2][D / 32], const Man
 
 __device__ __forceinline__ _Float16 half_of(uint32_t w, bool upper) { return __builtin_bit_cast(half2v, w)[upper ? 1 : 0]; }
 
-template <int D, int CT, int kParts>
+template <int D, int CT, bool kCentred>
 __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)[2], int base, const Queries<D, CT>& q, const int (&see)[CT], int see_all, int len, State<D, CT>& st,
                                         half8 (&p)[CT], int g) {
     const bool edge = base + kCacheBlock > see_all;
@@ -282,8 +288,7 @@ __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)
             for (int i = 0; i < 4; ++i) step[tt][i] = base + tt * 16 + 4 * g + i < len ? step[tt][i] : 0u;
     }
     // A quarter of the upper byte of an fp16 is its exponent field and two bits more.  The lane's largest step stands for its eight:
-    // that makes weights smaller than they could be by as much as the steps differ, which is taken up to 2^6 (fp16 has them
-    // in full down to 2^-14 of the largest).  Beyond that every token is looked at with its own.
+    // that makes weights smaller than they could be by as much as the steps differ, which is taken up to 2^6.  Beyond that every token is looked at with its own.
     uint32_t most = 0, least = 0xffffffffu;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
@@ -327,7 +332,7 @@ __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)
             const float m = __builtin_fmaxf(st.m[ct], max_rows(top)), f = __builtin_amdgcn_exp2f(st.m[ct] - m);
             st.m[ct] = m;
             st.l[ct] *= f;
-            st.eight[ct] *= f;
+            if constexpr (!kCentred) st.eight[ct] *= f;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] *= f;
         }
@@ -342,16 +347,18 @@ __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)
     }
 }
 
-template <int D, int CT>
+template <int D, int CT, bool kCentred>
 __device__ __forceinline__ void products(const u32x4 (&v)[D / 64], const half8 (&p)[CT], State<D, CT>& st) {
-    const half8 eight = as_halves(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
+    const half8 eight = as_halves(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u), upper_eight = as_halves(0x00800080u, 0x00800080u, 0x00800080u, 0x00800080u);
+    if constexpr (!kCentred)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) st.eight[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p[ct], st.eight[ct], 0, 0, 0);
+        for (int ct = 0; ct < CT; ++ct) st.eight[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p[ct], st.eight[ct], 0, 0, 0);
 #pragma unroll
     for (int h = 0; h < D / 64; ++h)
 #pragma unroll
         for (int pp = 0; pp < 2; ++pp) {
-            const half8 lo = value_operand_low(v[h][2 * pp], v[h][2 * pp + 1]), hi = value_operand_high(v[h][2 * pp], v[h][2 * pp + 1]);
+            half8 lo = value_operand_low(v[h][2 * pp], v[h][2 * pp + 1]), hi = value_operand_high(v[h][2 * pp], v[h][2 * pp + 1]);
+            if constexpr (kCentred) lo -= eight, hi -= upper_eight;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 st.o[4 * h + 2 * pp][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, p[ct], st.o[4 * h + 2 * pp][ct], 0, 0, 0);
@@ -420,7 +427,7 @@ __device__ __forceinline__ float across(float v, int which) {
 
 template <int D, int CT, int kWaves, Share kShare, int kParts>
 __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cache_attention_kernel(const AttnArgs a) {
-    constexpr bool kOwn = kShare == Share::none;
+    constexpr bool kOwn = kShare == Share::none, kCentred = !kOwn && kWaves < 16;
     typedef Lds<D, CT, kWaves, kShare, kParts> L;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     // heads fastest: with eight heads each die keeps to one, and its cache to that head's blocks
@@ -519,12 +526,12 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
                 half8 p[CT];
                 // (ahead of others' products: the vector ALU is what a unit has least of.  A chunk of 512 rows of 16500 tokens 365 -> 356 us)
                 __builtin_amdgcn_s_setprio(1);
-                weights<D, CT, kParts>(s, r.s, now.base, q, see, see_all, sq.len, st, p, g);
+                weights<D, CT, kCentred>(s, r.s, now.base, q, see, see_all, sq.len, st, p, g);
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_setprio(0);
                 load_steps<D>(next.at, r.s, lane);
                 __builtin_amdgcn_sched_barrier(0);
-                products<D, CT>(r.v, p, st);
+                products<D, CT, kCentred>(r.v, p, st);
                 __builtin_amdgcn_sched_barrier(0);
                 load_values<D>(next.at, r.v, lane);
                 __builtin_amdgcn_sched_barrier(0);
@@ -539,7 +546,10 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
         for (int ct = 0; ct < CT; ++ct) {
             st.l[ct] = sum_rows(st.l[ct]);
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) st.o[c][ct] = c % 2 == 0 ? (st.o[c][ct] - st.eight[ct]) * 16777216.f : (st.o[c][ct] - st.eight[ct] * 16.f) * 1048576.f;
+            for (int c = 0; c < D / 16; ++c) {
+                if constexpr (!kCentred) st.o[c][ct] -= c % 2 == 0 ? st.eight[ct] : st.eight[ct] * 16.f;
+                st.o[c][ct] *= c % 2 == 0 ? 16777216.f : 1048576.f;
+            }
         }
         if constexpr (!kOwn) {
             // Every wavefront leaves its sums.  A row is joined by a wavefront, D / 8 lanes a part.
@@ -773,7 +783,7 @@ int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStre
         if constexpr (D <= 128) wide = p.wide;
         if (!wide) rc = start<D, 1, 4, Share::blocks, 2>(a, grid, st);
         if constexpr (D <= 128)
-            if (wide) rc = start<D, 1, 16, Share::blocks, 1>(a, grid, st);
+            if (wide) rc = start<D, 1, 16, Share::blocks, 2>(a, grid, st);
     }
     if (rc != 0 || p.splits <= 1) return rc;
     int groups = 1;
