@@ -16,7 +16,7 @@
 // heads with the sines that it has worked out once.
 //
 // Measured: 11385 tokens, 64 normed query heads and 8 kv heads of 128, half of each rotated, fp16 (440 MB) 99 us, 4.4 TB/s; the
-// arithmetic in 64 bits takes the vector ALU for 72 % of that time, so neither the memory (a copy: 5.2 TB/s) nor the ALU
+// arithmetic in 64 bits takes the vector ALU for 71 % of that time, so neither the memory (a copy: 5.2 TB/s) nor the ALU
 // is far away.  One token 4.4 us, most of it a launch and two loads that wait for each other (position, then row).
 #include <type_traits>
 
@@ -421,7 +421,7 @@ __device__ __forceinline__ void value_pairs(const unsigned char* at, int shift, 
 // tokens beside each other, whole blocks go through LDS: listed rows are mostly neighbours, so 32 of them lie in one block or
 // two.  Where they do not, a lane gathers its eight bytes from memory.
 // Memory bounds it, the stores before all (fp16: 0.52 bytes in, 2 out a value; stored past the caches, nothing reads them
-// soon): 32768 tokens of 8 heads of 128, 169 MB, 33 us, 5.1 TB/s where a copy reaches 5.2.  The vector ALU is busy for 74 % of it.
+// soon): 32768 tokens of 8 heads of 128, 169 MB, 33 us, 5.1 TB/s where a copy reaches 5.2.  The vector ALU is busy for 76 % of it.
 template <int D, typename Out>
 __global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
     constexpr int kRows = Rows<D>::kRows, kChunks = D, kHalf = 1024 + 64;  // 16-byte chunks of a block's values; LDS bytes of 64 channels

@@ -17,11 +17,13 @@
 //
 // What bounds it.  Few rows: the stream of blocks -- 16 sequences of 1500 to 2500 tokens, 32 heads of 128 with one row each, 138 MB, in
 // 31 us, 4.5 TB/s (a copy: 5.2); one of 131072 tokens, 8 kv heads, in 25 us and 5 for the join.  A wavefront waits for memory
-// for 40 % of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four or eight a SIMD),
-// or two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
+// for a third of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four a SIMD), or
+// two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
 // 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (63 and 33 %
 // of it): 512 rows of 64 heads over 16500 tokens 355 us, 770 TFLOP/s.  Unpacking once for four wavefronts into LDS saves a
-// third of the vector instructions and took 340 to 385 us: it leaves room for no more wavefronts, and they wait for each other.
+// third of the vector instructions and took 345 to 385 us, other sizes 5 % more than
+// this: it leaves room for few more wavefronts, and they wait for each other.  (The older of two workgroups on a unit takes 270 us, the younger
+// 355; one of eight wavefronts that keep step takes as long.)
 #include "itq3s_attention.h"
 #include "itq3s_cache.h"
 
