@@ -480,6 +480,85 @@ def test_prompts_do_not_see_each_other(gpu):
     assert torch.equal(a[:40], b[:40]) and torch.equal(a[97:], b[97:]) and bool(torch.isnan(b[40:97]).all())
 
 
+@pytest.mark.parametrize("D,q_heads,kv_heads,lens,causal", [(64, 32, 32, [1100, 40], True), (64, 32, 32, [900], False), (256, 16, 8, [2100, 7], True), (256, 8, 8, [1400, 600], False), (128, 8, 8, [3100], True)])
+def test_prompt_attention_of_many_rows(gpu, D, q_heads, kv_heads, lens, causal):
+    """Enough tiles for workgroups of four wavefronts, for every head dimension; a sample of the rows."""
+    torch, binding = gpu
+    rng = np.random.default_rng(D + lens[0])
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T, G = int(starts[-1]), q_heads // kv_heads
+    q, k, v = rows(rng, T, q_heads, D, "f16", outliers=False), rows(rng, T, kv_heads, D, "f16"), rows(rng, T, kv_heads, D, "f16")
+    g = binding.itq3s_prompt_attention(dev(torch, q), dev(torch, k), dev(torch, v), D, dev(torch, starts), max_len=max(lens), causal=causal).double().cpu().numpy()
+    q, k, v, g = (x.astype(np.float64).reshape(T, -1, D) for x in (q, k, v, g))
+    for a, b in zip(starts[:-1], starts[1:]):
+        for i in {int(a), int(b) - 1, *(int(x) for x in rng.integers(a, b, 20))}:
+            for h in rng.choice(q_heads, 4, replace=False):
+                end = i + 1 if causal else b
+                o, weight, reach = plain.attend(q[i, h], k[a:end, h // G], v[a:end, h // G], D**-0.5)
+                assert np.linalg.norm(g[i, h] - o) <= plain.bound(o, weight, reach)
+
+
+WAYS = [
+    # q_heads, kv_heads, rows, tokens: which way the work is cut (a unit's count of the card that decides is 256)
+    (8, 2, [1, 1, 1], [400, 130, 77]),        # sixteen wavefronts a sequence
+    (8, 2, [1], [9000]),                      # parts of a sequence
+    (8, 2, [3, 1, 4], [2500, 31, 6000]),      # tiles of 16 rows in parts, sequences of different lengths
+    (8, 1, [4, 3], [3000, 500]),              # two tiles a workgroup
+    (8, 1, [12, 2], [2000, 50]),              # several tiles, of 16 rows each
+    (64, 8, [300], [2100]),                   # rows of their own, in parts
+    (64, 8, [40, 1, 0, 280], [70, 3, 9, 300]),
+]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_heads,kv_heads,n,lens", WAYS)
+def test_every_way_of_cutting_up_cache_attention(gpu, q_heads, kv_heads, n, lens, D):
+    """A sample of rows against 64 bits on what the cache holds."""
+    torch, binding = gpu
+    rng = np.random.default_rng(D + sum(lens))
+    page, G, S = 64, q_heads // kv_heads, len(lens)
+    starts = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    T, counts = int(starts[-1]), [-(-x // page) for x in lens]
+    table, order, at = np.zeros((S, max(counts)), dtype=np.int32), rng.permutation(sum(counts)), 0
+    for s in range(S):
+        table[s, : counts[s]], at = order[at : at + counts[s]], at + counts[s]
+    slots = [table[s, np.arange(lens[s]) // page].astype(np.int64) * page + np.arange(lens[s]) % page for s in range(S)]
+    cache, total = binding.alloc_cache(sum(counts), page, kv_heads, D), sum(lens)
+    k, v, q = rows(rng, total, kv_heads, D, "f16"), rows(rng, total, kv_heads, D, "f16"), rows(rng, T, q_heads, D, "f16", outliers=False)
+    all_slots = dev(torch, np.concatenate(slots))
+    binding.itq3s_cache_append(None, dev(torch, k), dev(torch, v), None, None, cache, all_slots)
+    K, V = (x.double().cpu().numpy().reshape(total, kv_heads, D) for x in binding.itq3s_cache_read(cache, all_slots, dtype=torch.float32))
+    args = (dev(torch, q), cache, dev(torch, starts), dev(torch, np.array(lens, dtype=np.int32)), dev(torch, table))
+    out = binding.itq3s_cache_attention(*args, max_q=max(n), max_kv=max(lens))
+    assert torch.equal(out, binding.itq3s_cache_attention(*args, max_q=max(n), max_kv=max(lens)))
+    g, q = out.double().cpu().numpy().reshape(T, q_heads, D), q.astype(np.float64).reshape(T, q_heads, D)
+    first = np.concatenate([[0], np.cumsum(lens)])
+    for s in range(S):
+        for i in sorted({0, n[s] - 1, *(int(x) for x in rng.integers(0, max(n[s], 1), 12))} & set(range(n[s]))):
+            see = max(0, lens[s] - n[s] + i + 1)
+            for h in rng.choice(q_heads, min(q_heads, 6), replace=False):
+                kk, vv, x = K[first[s] : first[s] + see, h // G], V[first[s] : first[s] + see, h // G], q[starts[s] + i, h]
+                o, weight, _ = plain.attend(x, kk, vv, D**-0.5)
+                reach = D**-0.5 * float((np.abs(plain.turned(kk)) @ np.abs(plain.turned(x))).max()) if see else 0.0
+                assert np.linalg.norm(g[starts[s] + i, h] - o) <= plain.bound(o, weight, reach), (s, i, h)
+
+
+def test_positions_at_their_ends(gpu):
+    """Angles of positions up to 2^31 - 1, negative ones, frequencies above 1."""
+    torch, binding = gpu
+    rng = np.random.default_rng(31)
+    D, T = 128, 9
+    pos = np.array([0, 1, -1, 2**31 - 1, -(2**31), 10**9 + 7, -12345678, 2**24 + 1, 131071], dtype=np.int32)
+    x = rows(rng, T, 2, D, "f32")
+    for interleaved in (False, True):
+        freq = np.concatenate([binding.itq3s_rope_frequencies(2 * 60, 1e6).numpy(), [3.0, 0.0, 1e-300, 0.7853981633974483]])
+        got, _ = binding.itq3s_cache_append(dev(torch, x), None, None, dev(torch, pos), dev(torch, freq), head_dim=D, interleaved=interleaved, dtype=torch.float32)
+        want = plain.rotated(x, D, positions=pos, freq=freq, interleaved=interleaved)
+        pair = np.abs(x.astype(np.float64)).max()
+        # cosine and sine round to fp32, two products and a sum: four roundings of a pair's magnitude
+        assert np.abs(got.double().cpu().numpy() - want).max() <= 4 * 2.0**-24 * 2 * pair
+
+
 # ---- sizes at their ends
 
 
