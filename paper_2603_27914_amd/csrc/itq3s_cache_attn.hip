@@ -20,7 +20,7 @@
 // for a third of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four a SIMD), or
 // two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
 // 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (63 and 33 %
-// of it): 512 rows of 64 heads over 16500 tokens 355 us, 770 TFLOP/s.  Unpacking once for four wavefronts into LDS saves a
+// of it): 512 rows of 64 heads over 16500 tokens 351 us, 776 TFLOP/s.  Unpacking once for four wavefronts into LDS saves a
 // third of the vector instructions and took 345 to 385 us, other sizes 5 % more than
 // this: it leaves room for few more wavefronts, and they wait for each other.  (The older of two workgroups on a unit takes 270 us, the younger
 // 355; one of eight wavefronts that keep step takes as long.)
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
 
 // Joins the parts of rows whose sequence was split: D / 8 lanes a part, `lanes` groups of them a row (a power of two up to a
 // workgroup's), the groups of a row beside each other.  64 rows of 64 parts 5 us, of which a launch is half; 32768 rows of two, 34 MB,
-// 13 us.
+// 9 us.
 template <int D>
 __global__ void __launch_bounds__(256) combine_kernel(const AttnArgs a, int groups_of_row) {
     constexpr int kLanes = D / 8, kGroups = 256 / kLanes;
@@ -789,7 +789,7 @@ int start(const AttnArgs& a, const Plan& p, int64_t grid, int64_t max_q, hipStre
     }
     if (rc != 0 || p.splits <= 1) return rc;
     int groups = 1;
-    while (2 * groups <= p.splits && groups < 2048 / D) groups *= 2;
+    while (4 * groups < p.splits && groups < 2048 / D) groups *= 2;  // (four parts a group are one round of loads)
     const int64_t at_once = 2048 / D / groups, rows = (max_q * a.q_heads + at_once - 1) / at_once;
     combine_kernel<D><<<dim3((unsigned)a.seqs, (unsigned)(rows < 65535 ? rows : 65535)), dim3(256), 0, st>>>(a, groups);
     return hipGetLastError() == hipSuccess ? 0 : -6;
