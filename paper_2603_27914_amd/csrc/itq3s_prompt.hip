@@ -9,7 +9,8 @@
 //
 // Tiles of 32 tokens are copied to LDS by the memory pipe, a tile ahead, rows as in memory, 16-byte chunks permuted within a
 // row against bank conflicts (by the address that each lane copies from); V^T is read with the transposing LDS read.
-// Three workgroups of four wavefronts a compute unit: nothing in a wavefront overlaps its products with its exponentials, the
+// Few rows leave compute units with little: there two wavefronts share the tokens of the same rows and join in LDS.
+// Many: three workgroups of four wavefronts a compute unit: nothing in a wavefront overlaps its products with its exponentials, the
 // others do.  (One wavefront a SIMD with 64 rows, which reads LDS half as often, and its two halves interleaved by hand: 606
 // us where this takes 546, 8192 tokens, 32 query and 8 kv heads of 128.)  That is 1.03 PFLOP/s, where a matrix product of
 // 8192 x 8192 x 8192 reaches 1.21; the matrix pipes are busy for 58 % of the time, the vector ALU for 46 to 53 %, and the clock is down
@@ -83,14 +84,19 @@ __device__ __forceinline__ u32x4 rows_descriptor(const _Float16* p, int64_t byte
     return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, (uint32_t)bytes, 0x00027000u};
 }
 
-template <int D, int kWaves>
-__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : D == 128 ? 3 : kWaves / 2, D == 64 ? 4 : D == 128 ? 3 : kWaves / 2))) prompt_kernel(const PromptArgs a) {
-    constexpr int kThreads = 64 * kWaves, kChunks = kTile * D / 8 / kThreads, kTileBytes = kTile * D * 2, kValues = 2 * kTileBytes;
+// Wavefronts a SIMD: what LDS has room for, three for 128 channels.
+constexpr int waves_of_simd(int D, int waves, int parts) { return D == 64 ? 4 : parts == 2 ? (D == 128 ? 2 : 1) : D == 128 ? 3 : waves / 2; }
+
+// kParts = 2: the wavefronts of one half take the tiles 0, 2, 4, ..., the others, with the same rows, 1, 3, 5, ..., and join in the end.
+template <int D, int kWaves, int kParts>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_of_simd(D, kWaves, kParts), waves_of_simd(D, kWaves, kParts)))) prompt_kernel(const PromptArgs a) {
+    constexpr int kThreads = 64 * kWaves, kTokens = kTile * kParts, kChunks = kTokens * D / 8 / kThreads, kTileBytes = kTile * D * 2, kStepBytes = kParts * kTileBytes, kValues = 2 * kStepBytes;
     constexpr int kStep = kThreads * 8 / D;  // rows between a thread's chunks
-    __shared__ __align__(1024) unsigned char lds[4 * kTileBytes];  // two tiles of keys, two of values
+    __shared__ __align__(1024) unsigned char lds[4 * kStepBytes];  // keys of two steps, values of two
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = lane_id(), hi = lane >> 5, col = lane & 31;
-    const uint32_t k_place = key_place<D>(lane), v_place = value_place<D>(lane) + kValues;
+    const int part = kParts == 1 ? 0 : wave / (kWaves / kParts), group = kParts == 1 ? wave : wave % (kWaves / kParts);  // which tiles and which rows
+    const uint32_t k_place = key_place<D>(lane) + part * kTileBytes, v_place = value_place<D>(lane) + kValues + part * kTileBytes;
     int id = blockIdx.x;
     const int head = id % a.kv_heads;
     id /= a.kv_heads;
@@ -99,13 +105,13 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     first = first < 0 ? 0 : first > a.T ? a.T : first;
     end = end < first ? first : end > a.T ? a.T : end;
     const int len = end - first, total = len * a.group;
-    constexpr int kRows = 32 * kWaves;
+    constexpr int kRows = 32 * kWaves / kParts;
     const int count = (total + kRows - 1) / kRows;
     const _Float16* const kb = a.K + (int64_t)first * a.ldk + (int64_t)head * D;
     const _Float16* const vb = a.V + (int64_t)first * a.ldv + (int64_t)head * D;
     // the last rows have the most to see: they begin
     for (int tile = count - 1 - id / a.seqs; tile >= 0; tile -= a.tiles) {
-        const int row0 = tile * kRows + wave * 32, row = row0 + col;
+        const int row0 = tile * kRows + group * 32, row = row0 + col;
         const int last_row = (tile + 1) * kRows < total ? (tile + 1) * kRows - 1 : total - 1;
         const int tokens = a.causal ? last_row / a.group + 1 : len;  // that the workgroup needs
         const int my_last = row0 + 32 < total ? row0 + 31 : total - 1;
@@ -116,10 +122,10 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
         const int r = tid / (D / 8), c = tid % (D / 8);
         const int k_row = (int)(r * a.ldk * 2), v_row = (int)(r * a.ldv * 2), k_chunk = (c ^ k_mix<D>(r)) * 16, v_chunk = (c ^ v_mix<D>(r)) * 16;
         auto load = [&](int t0, int buffer) {  // (rows behind the sequence are another's, or nothing: zeros)
-            const int rows = len - t0 < kTile ? len - t0 : kTile;
+            const int rows = len - t0 < kTokens ? len - t0 : kTokens;
             const u32x4 kd = rows_descriptor(kb + t0 * a.ldk, rows > 0 ? ((rows - 1) * a.ldk + D) * 2 : 0);
             const u32x4 vd = rows_descriptor(vb + t0 * a.ldv, rows > 0 ? ((rows - 1) * a.ldv + D) * 2 : 0);
-            const uint32_t to = lds_base + (uint32_t)(buffer * kTileBytes + wave * 1024);
+            const uint32_t to = lds_base + (uint32_t)(buffer * kStepBytes + wave * 1024);
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) {
                 copy_to_lds(kd, k_row + (int)(u * kStep * 2 * a.ldk) + (k_chunk ^ k_mix<D>(u * kStep) * 16), to + u * kThreads * 16);
@@ -143,11 +149,12 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
             for (int y = 0; y < 16; ++y) o[x][y] = 0.f;
         int buffer = 0;
-        for (int t0 = 0; t0 < tokens; t0 += kTile, buffer ^= 1) {
-            sync_copies();  // this tile is there, and the other one's place is free
-            load(t0 + kTile, buffer ^ 1);
+        for (int step = 0; step < tokens; step += kTokens, buffer ^= 1) {
+            sync_copies();  // this step's tiles are there, and the others' place is free
+            load(step + kTokens, buffer ^ 1);
+            const int t0 = step + part * kTile;
             if (t0 >= mine) continue;
-            const uint32_t ka = k_place + buffer * kTileBytes, va = v_place + buffer * kTileBytes;
+            const uint32_t ka = k_place + buffer * kStepBytes, va = v_place + buffer * kStepBytes;
             floatx16 s;
 #pragma unroll
             for (int x = 0; x < 16; ++x) s[x] = 0.f;
@@ -183,6 +190,30 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
                 for (int x = 0; x < D / 32; ++x) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_part<D>(lds, va, k, x), p[k], o[x], 0, 0, 0);
         }
         l += xor_lane_f32(l, 32);
+        if constexpr (kParts == 2) {
+            sync_copies();
+            floatx4* const meet = reinterpret_cast<floatx4*>(lds) + group * ((D / 8 + 1) * 64) + lane;
+            if (part == 1) {
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) meet[(4 * x + y) * 64] = floatx4{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
+                meet[D / 8 * 64] = floatx4{m, l, 0.f, 0.f};
+            }
+            sync_copies();
+            if (part == 1) continue;
+            const floatx4 ml = meet[D / 8 * 64];
+            const float n = __builtin_fmaxf(m, ml[0]), f0 = __builtin_amdgcn_exp2f(m - n), f1 = __builtin_amdgcn_exp2f(ml[0] - n);
+            l = l * f0 + ml[1] * f1;
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const floatx4 v = meet[(4 * x + y) * 64];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[x][4 * y + z] = o[x][4 * y + z] * f0 + v[z] * f1;
+                }
+        }
         const float f = l == 0.f ? 0.f : 1.f / l;
         if (there) {
             _Float16* const out = a.out + (int64_t)(first + i) * a.ldo + (int64_t)hq * D + 4 * hi;
@@ -196,21 +227,26 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     sync_copies();  // (the copies behind the last tile are into this workgroup's LDS)
 }
 
-template <int D, int kWaves>
+template <int D, int kWaves, int kParts>
 int start(PromptArgs a, int64_t max_len, hipStream_t st) {
-    const int64_t units = (int64_t)a.seqs * a.kv_heads, tiles = most_tiles((max_len * a.group + 32 * kWaves - 1) / (32 * kWaves), units), grid = tiles * units;
+    constexpr int kRows = 32 * kWaves / kParts;
+    const int64_t units = (int64_t)a.seqs * a.kv_heads, tiles = most_tiles((max_len * a.group + kRows - 1) / kRows, units), grid = tiles * units;
     a.tiles = (int)tiles;
-    prompt_kernel<D, kWaves><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, st>>>(a);
+    prompt_kernel<D, kWaves, kParts><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, st>>>(a);
     return hipGetLastError() == hipSuccess ? 0 : -6;
 }
 template <int D>
 int start(const PromptArgs& a, int64_t max_len, hipStream_t st) {
-    // Four wavefronts share a tile, or two where four would leave compute units without a workgroup: us with two and with four, 32 query
-    // and 8 kv heads of 128, one sequence of 250 tokens 11.1 and 12.0, of 1000 (the border) 29.0 and 30.0, of 2000 57.3 and 53.6,
-    // 7 of 700 57.5 and 50.8; 16 and 8 heads of 256, 1000 tokens 47.7 and 50.0, 7 of 700 73.8 and 52.3.  (There are rows for so many
-    // tiles at most, whatever max_len says.)
-    const int64_t tiles = (max_len * a.group + 127) / 128 * a.seqs, all = (int64_t)a.T * a.group / 128 + a.seqs;
-    return (tiles < all ? tiles : all) * a.kv_heads < cu_count() ? start<D, 2>(a, max_len, st) : start<D, 4>(a, max_len, st);
+    // Workgroups of four wavefronts with rows of their own.  (There are rows for so many at most, whatever max_len says.)
+    const int64_t tiles = (max_len * a.group + 127) / 128 * a.seqs, all = (int64_t)a.T * a.group / 128 + a.seqs, full = (tiles < all ? tiles : all) * a.kv_heads, cus = cu_count();
+    // Where they are fewer than compute units (twice as many for 64 channels, whose LDS has room for more), the last rows' way through
+    // their tokens is what a call takes: two wavefronts share it, if there are enough tokens to share.  us with four, two that share
+    // rows' tokens (and two with rows of their own): 32 query and 8 kv heads of 128, one sequence of 60 tokens 8.0, 7.7 (7.0), 250
+    // 12.0, 9.9 (11.1), 1000 30.0, 22.4 (28.6), 2000 53.0, 52.4 (56.5); 4 of 250 13.9, 13.6 (12.9); 16 and 4 heads of 64, 2000
+    // tokens 37.8, 23.6 (37.5), 4000 68.8, 50.2 (69.4), 7 of 700 19.8, 20.5; 16 and 8 of 256, 2000 91.8, 67.8 (93.5), 4000 187, 216.
+    if (full <= (D == 64 ? 2 : 1) * cus && max_len >= 192 && max_len * cus >= 384 * full) return start<D, 4, 2>(a, max_len, st);
+    // Else two wavefronts a workgroup where four would leave compute units without one.
+    return full < cus ? start<D, 2, 1>(a, max_len, st) : start<D, 4, 1>(a, max_len, st);
 }
 
 }  // namespace
