@@ -244,9 +244,12 @@ int start(const PromptArgs& a, int64_t max_len, hipStream_t st) {
     // rows' tokens (and two with rows of their own): 32 query and 8 kv heads of 128, one sequence of 60 tokens 8.0, 7.7 (7.0), 250
     // 12.0, 9.9 (11.1), 1000 30.0, 22.4 (28.6), 2000 53.0, 52.4 (56.5); 4 of 250 13.9, 13.6 (12.9); 16 and 4 heads of 64, 2000
     // tokens 37.8, 23.6 (37.5), 4000 68.8, 50.2 (69.4), 7 of 700 19.8, 20.5; 16 and 8 of 256, 2000 91.8, 67.8 (93.5), 4000 187, 216.
-    if (full <= (D == 64 ? 2 : 1) * cus && max_len >= 192 && max_len * cus >= 384 * full) return start<D, 4, 2>(a, max_len, st);
+    // Without a mask every row's way is the same, and they have to fit at once, two for one, which 256 channels halve: 1000 tokens
+    // 53.0, 36.0 (48.7), 1403 69.3, 80.5 (77.8).
+    const bool enough = max_len >= 192 && max_len * cus >= 384 * full;
+    if (enough && 2 * full <= (D == 64 ? 4 : D == 256 && !a.causal ? 1 : 2) * cus) return start<D, 4, 2>(a, max_len, st);
     // Else two wavefronts a workgroup where four would leave compute units without one.
-    return full < cus ? start<D, 2, 1>(a, max_len, st) : start<D, 4, 1>(a, max_len, st);
+    return full < cus && !enough ? start<D, 2, 1>(a, max_len, st) : start<D, 4, 1>(a, max_len, st);
 }
 
 }  // namespace
