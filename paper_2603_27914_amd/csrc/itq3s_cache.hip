@@ -213,7 +213,8 @@ __device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8]
     if (bad) s = (_Float16)0.f;
     const double step = (double)(float)s * kRootD<D>, inv = step > 0.0 ? 1.0 / step : 0.0;
     int d[8];
-    // The nearest whole number, from the low bits of w / step + 1.5 2^52; it is right where the remainder stays clear of half a step.
+    // The nearest whole number, from the low bits of w / step + 1.5 2^52; it is right where the remainder stays clear of half a step, and
+    // the number within 32 bits: it is unless the step was cut to fp16's largest.
     constexpr double kWhole = 6755399441055744.0;
     double rest = 0.0;
 #pragma unroll
@@ -222,7 +223,7 @@ __device__ __forceinline__ void quantize_row(const AppendArgs& a, double (&v)[8]
         rest = __builtin_fmax(rest, __builtin_fabs(__builtin_fma(kWhole - q, step, v[j])));
         d[j] = __double2loint(q);
     }
-    if (__builtin_amdgcn_ballot_w64(!(rest < step * (0.5 - 0x1p-40))) != 0) {  // a border (or a step of 0) in the wavefront
+    if (__builtin_amdgcn_ballot_w64(sat || !(rest < step * (0.5 - 0x1p-40))) != 0) {  // such a row, a border or a step of 0 in the wavefront
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             // floor(w / step + 1/2): by the reciprocal, then set right by the remainder, whose sign is exact
