@@ -50,3 +50,99 @@ def test_rows_far_beyond_the_largest_step_keep_their_signs(gpu, D, normed):
     want.write(slots, plain.rotated(k.reshape(T, -1), D, weight).reshape(T, H, D), v.astype(np.float64))
     assert np.array_equal(cache.data.cpu().numpy(), want.data)
     assert int(flags.item()) == binding.FLAG_SCALE_SAT
+
+
+# ---- scores of every size
+
+
+SCALES = [1e4, -1e6, 1e9, 2.0**40]
+
+
+def check_row(got, q, k, v, scale, reach, slack):
+    """One row over the tokens that it sees, where scores may be of any size: 1 if it could be checked.
+
+    A score may be off by `slack` of its reach (operands' roundings, sums).  Where all scores are small that is what bound() prices.  Where
+    the largest leads by more than both scores may be off, and by 50 beside that (e^-50 is below any rounding), it alone has weight, with those
+    equal to it bit for bit (equal keys): their weights are the same number, so no error of the score enters."""
+    s = k @ q
+    if abs(scale) * reach <= 500:
+        o, weight, _ = plain.attend(q, k, v, scale)
+        assert np.linalg.norm(got - o) <= plain.bound(o, weight, abs(scale) * reach)
+        return 1
+    s = s * np.sign(scale)
+    same = (k == k[s.argmax()]).all(axis=1)
+    if len(k) > same.sum() and s.max() - s[~same].max() <= 2 * slack * reach + 50 / abs(scale):
+        return 0
+    o, weight = v[same].mean(axis=0), float(np.sqrt((v[same] ** 2).sum(axis=1)).mean())
+    assert np.linalg.norm(got - o) <= plain.bound(o, weight, 0.0), (s.max() * abs(scale), np.linalg.norm(got - o))
+    return 1
+
+
+def big_rows(rng, T, heads, D):
+    """Rows of which some are 2^10 and 2^20 times smaller"""
+    return (rng.standard_normal((T, heads, D)) * 2.0 ** rng.choice([0, 0, 0, -10, -20], (T, heads, 1))).astype(np.float16)
+
+
+PROMPTS = [
+    # q_heads, kv_heads, lengths, causal: two wavefronts a workgroup, two that share rows' tokens, four
+    (4, 2, [1, 2, 33, 70], True),
+    (2, 2, [300], True),
+    (4, 1, [250, 40], False),
+    (64, 8, [530, 12, 300], True),
+]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_heads,kv_heads,lens,causal", PROMPTS)
+def test_prompt_scores_of_every_size(gpu, q_heads, kv_heads, lens, causal, D, scale):
+    torch, binding = gpu
+    rng = np.random.default_rng(D + q_heads)
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T, G = int(starts[-1]), q_heads // kv_heads
+    q, k, v = big_rows(rng, T, q_heads, D), rng.standard_normal((T, kv_heads, D)).astype(np.float16), rng.standard_normal((T, kv_heads, D)).astype(np.float16)
+    k[rng.permutation(T)[: T // 3]] = k[rng.integers(0, T, T // 3)]  # equal keys
+    got = binding.itq3s_prompt_attention(*(dev(torch, x.reshape(T, -1)) for x in (q, k, v)), D, dev(torch, starts), causal=causal, scale=scale)
+    got, q, k, v = (x.astype(np.float64) for x in (got.cpu().numpy().reshape(T, q_heads, D), q, k, v))
+    done = []
+    for a, b in zip(starts[:-1], starts[1:]):
+        for i in range(a, b) if b - a < 80 else sorted({int(a), int(b) - 1, *(int(x) for x in rng.integers(a, b, 30))}):
+            end = i + 1 if causal else b
+            for h in range(q_heads) if q_heads < 10 else rng.choice(q_heads, 4, replace=False):
+                kk = k[a:end, h // G]
+                # products of fp16 are exact; D sums of fp32, cut or rounded
+                done.append(check_row(got[i, h], q[i, h], kk, v[a:end, h // G], scale, float((np.abs(kk) @ np.abs(q[i, h])).max()), D * 2.0**-23))
+    assert np.mean(done) > 0.6
+
+
+@pytest.mark.parametrize("factor", [3000.0, 8000.0, 20000.0])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_prompts_of_one_token_give_its_value(gpu, D, factor):
+    """The default scale, q and k as large as fp16 has them: scores of 2^27 to 2^37."""
+    torch, binding = gpu
+    rng = np.random.default_rng(int(factor))
+    T, H = 200, 2
+    q = (rng.standard_normal((T, H * D)) * factor).clip(-65504, 65504).astype(np.float16)
+    q[0], q[1] = 8000.0, -factor
+    k, v = np.where(rng.random((T, 1)) < 0.5, 1, -1).astype(np.float16) * q, rng.standard_normal((T, H * D)).astype(np.float16)
+    got = binding.itq3s_prompt_attention(*(dev(torch, x) for x in (q, k, v)), D, dev(torch, np.arange(T + 1, dtype=np.int32)), max_len=1).double().cpu().numpy()
+    v = v.astype(np.float64)
+    # one weight, rounded to fp16, against itself in fp32, and the result's rounding
+    assert np.all(np.abs(got - v) <= 2.02 * 2.0**-11 * np.abs(v) + 2.0**-25)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("scale", [0.25, 0.5, 1.0, 2.0, 4.0])
+@pytest.mark.parametrize("T,heads", [(60, 1), (400, 1), (200, 64)])
+def test_prompt_scores_that_are_large_and_close(gpu, T, heads, scale, sign):
+    """Scores 2^23 + j times the scale, j from 0 to 5, which are exact in fp32: the weights are e^(j scale) all the same."""
+    torch, binding = gpu
+    rng = np.random.default_rng(T)
+    D = 64
+    q, k, v = np.zeros((T, heads, D)), np.zeros((T, 1, D)), rng.standard_normal((T, 1, D)).astype(np.float16)
+    q[..., 0], q[..., 1], k[..., 0], k[..., 1] = 2048.0 * sign, 1.0, 4096.0, rng.integers(0, 6, (T, 1))
+    got = binding.itq3s_prompt_attention(*(dev(torch, x.reshape(T, -1).astype(np.float16)) for x in (q, k, v)), D, dev(torch, np.array([0, T], dtype=np.int32)), scale=scale)
+    got, v = got.double().cpu().numpy().reshape(T, heads, D), v.astype(np.float64)
+    for i in range(T):
+        o, weight, _ = plain.attend(q[i, 0], k[: i + 1, 0], v[: i + 1, 0], scale)
+        assert np.linalg.norm(got[i] - o, axis=1).max() <= plain.bound(o, weight, 0.0)
