@@ -11,6 +11,9 @@
 // y + exponent(s_v): P' stays within fp16 whatever the steps are, and l = sum exp2(y - m) in fp32 has the range to follow.
 // m only moves when a row's weights would pass 2^15 (then O and l are scaled, weights up to 2^7 again): a block costs no rescaling
 // otherwise, and weights keep all of fp16's bits down to 2^-21 of a long row's largest.
+// Of large scores the step's exponent is lost in m, and y - m holds what m's rounding left: from 2^25 on a weight could be beyond
+// fp16.  So where a row passes 2^22 its reference is its largest score alone, before that is multiplied with the scale (State::far):
+// the difference comes first, and a weight is at most a step of values.
 //
 // Few rows: the wavefronts of a workgroup take blocks in turn and meet in LDS.  Many rows: each has its own rows.  A
 // long context is split over workgroups besides; combine_kernel joins the parts.
@@ -33,6 +36,7 @@ namespace {
 
 constexpr float kNoRow = -1e30f;    // reference of a row that has seen nothing
 constexpr float kHeadroom = 8.f;    // weights may grow by 2^8 before the reference moves
+constexpr float kFar = 4194304.f;   // 2^22: references beyond it are rounded by more than weights have room for
 constexpr int kExpBias = 21;        // s < 2^(E - 14) for an fp16 with exponent field E; weights take 2^7 of what fp16 has above 2^8
 constexpr int kMaxSplits = 256;
 
@@ -252,6 +256,8 @@ template <int D, int CT>
 struct State {
     floatx4 o[D / 16][CT], eight[CT];
     float m[CT], l[CT];
+    float far[CT];  // a row's reference is m + far * unit: one of them is 0, m where a score's size passes kFar
+    float room;     // how far scores may be above m: kHeadroom, or minus infinity (every block moves references) once a row is there
 };
 
 template <int D, int CT, int kParts>
@@ -330,9 +336,25 @@ __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)
                 for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, __builtin_fmaf((float)(step[tt][i] >> 24), 0.25f, x[tt][i] * unit));
             top -= (float)kExpBias;
         }
-        if (__builtin_amdgcn_ballot_w64(top > st.m[ct] + kHeadroom) != 0) {
-            const float m = __builtin_fmaxf(st.m[ct], max_rows(top)), f = __builtin_amdgcn_exp2f(st.m[ct] - m);
-            st.m[ct] = m;
+        if (__builtin_amdgcn_ballot_w64(top > st.m[ct] + st.room) != 0) {
+            float m = __builtin_fmaxf(__builtin_fmaf(st.far[ct], unit, st.m[ct]), max_rows(top)), far = 0.f;
+            if (st.room < 0.f || __builtin_amdgcn_ballot_w64(__builtin_fabsf(m) > kFar && m > 0.1f * kNoRow) != 0) {
+                asm volatile("");
+                st.room = -__builtin_inff();
+                float most_x = -__builtin_inff();
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) most_x = __builtin_fmaxf(most_x, x[tt][i]);
+                most_x = max_rows(most_x);
+                if (__builtin_fabsf(m) > kFar && m > 0.1f * kNoRow) m = 0.f, far = st.far[ct] != 0.f ? __builtin_fmaxf(st.far[ct], most_x) : most_x;
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[tt][i] -= far;
+            }
+            const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(st.far[ct] - far, unit, st.m[ct] - m));
+            st.m[ct] = m, st.far[ct] = far;
             st.l[ct] *= f;
             if constexpr (!kCentred) st.eight[ct] *= f;
 #pragma unroll
@@ -497,6 +519,7 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
         }
         __syncthreads();
         State<D, CT> st;
+        st.room = kHeadroom;
         Queries<D, CT> q;
         int see[CT];
 #pragma unroll
@@ -504,7 +527,7 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
             const int row = row0 + ct * 16 + col, v = sq.len - sq.rows + row / a.group + 1;
             see[ct] = row < total && v > 0 ? v : 0;
             load_queries<D, CT, kParts>(lds, queries + ((kOwn ? 0 : first_row) + ct * 16 + col) * kQueryPitch<D, kParts>, ct, q, g);
-            st.m[ct] = kNoRow, st.l[ct] = 0.f;
+            st.m[ct] = kNoRow, st.l[ct] = st.far[ct] = 0.f;
             st.eight[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st.o[c][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -547,6 +570,7 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             st.l[ct] = sum_rows(st.l[ct]);
+            st.m[ct] = __builtin_fmaf(st.far[ct], q.unit[ct], st.m[ct]);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
                 if constexpr (!kCentred) st.o[c][ct] -= c % 2 == 0 ? st.eight[ct] : st.eight[ct] * 16.f;

@@ -146,3 +146,74 @@ def test_prompt_scores_that_are_large_and_close(gpu, T, heads, scale, sign):
     for i in range(T):
         o, weight, _ = plain.attend(q[i, 0], k[: i + 1, 0], v[: i + 1, 0], scale)
         assert np.linalg.norm(got[i] - o, axis=1).max() <= plain.bound(o, weight, 0.0)
+
+
+WAYS = [
+    # q_heads, kv_heads, rows, tokens: sixteen wavefronts a sequence, parts of one, tiles of 16 rows in parts, two tiles a workgroup, rows of their own
+    (8, 2, [1, 1, 1], [200, 1, 77]),
+    (8, 1, [1], [6000]),
+    (8, 2, [3, 1, 4], [1500, 31, 600]),
+    (8, 1, [4, 3], [900, 500]),
+    (64, 8, [300, 40], [1400, 60]),
+]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_heads,kv_heads,n,lens", WAYS)
+def test_cache_scores_of_every_size(gpu, q_heads, kv_heads, n, lens, D, scale):
+    torch, binding = gpu
+    rng = np.random.default_rng(D + q_heads + len(n))
+    page, G, S, total = 64, q_heads // kv_heads, len(lens), sum(lens)
+    starts = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    T, counts, first = int(starts[-1]), [-(-x // page) for x in lens], np.concatenate([[0], np.cumsum(lens)])
+    table, at = np.zeros((S, max(counts)), dtype=np.int32), 0
+    for s in range(S):
+        table[s, : counts[s]], at = np.arange(at, at + counts[s]), at + counts[s]
+    slots = np.concatenate([table[s, np.arange(lens[s]) // page].astype(np.int64) * page + np.arange(lens[s]) % page for s in range(S)])
+    k, v = rng.standard_normal((total, kv_heads, D)), rng.standard_normal((total, kv_heads, D)) * 10.0 ** rng.uniform(-2, 2, (total, 1, 1))
+    k[rng.permutation(total)[: total // 3]] = k[rng.integers(0, total, total // 3)]  # equal keys
+    cache = binding.alloc_cache(at, page, kv_heads, D)
+    binding.itq3s_cache_append(None, *(dev(torch, x.reshape(total, -1).astype(np.float32)) for x in (k, v)), None, None, cache, dev(torch, slots))
+    k, v = (x.double().cpu().numpy().reshape(total, kv_heads, D) for x in binding.itq3s_cache_read(cache, dev(torch, slots), dtype=torch.float32))
+    q = big_rows(rng, T, q_heads, D)
+    out = binding.itq3s_cache_attention(dev(torch, q.reshape(T, -1)), cache, dev(torch, starts), dev(torch, np.array(lens, dtype=np.int32)), dev(torch, table), scale=scale, max_q=max(n), max_kv=max(lens))
+    got, q = out.double().cpu().numpy().reshape(T, q_heads, D), q.astype(np.float64)
+    done = []
+    for s in range(S):
+        for i in sorted({0, n[s] - 1, *(int(x) for x in rng.integers(0, n[s], 12))}):
+            see = max(0, lens[s] - n[s] + i + 1)
+            for h in range(q_heads) if q_heads < 10 else rng.choice(q_heads, 6, replace=False):
+                kk, vv = k[first[s] : first[s] + see, h // G], v[first[s] : first[s] + see, h // G]
+                reach = float((np.abs(plain.turned(kk)) @ np.abs(plain.turned(q[starts[s] + i, h]))).max()) if see else 0.0
+                if see:
+                    # H q rounds to fp16 once where rows are a wavefront's own
+                    done.append(check_row(got[starts[s] + i, h], q[starts[s] + i, h], kk, vv, scale, reach, 1.02 * 2.0**-11))
+                else:
+                    assert not got[starts[s] + i, h].any()
+    assert np.mean(done) > 0.6
+
+
+@pytest.mark.parametrize("factor", [3000.0, 20000.0])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows_of_one", [1, 40])
+def test_cached_sequences_of_one_token_give_its_value(gpu, rows_of_one, D, factor):
+    """The default scale, q and k as large as fp16 has them.  (Forty rows of a sequence of one token: all but the last see nothing.)"""
+    torch, binding = gpu
+    rng = np.random.default_rng(D)
+    S, G = 30, 4
+    k = (rng.standard_normal((S, 1, D)) * factor).clip(-65504, 65504).astype(np.float16)
+    v = (rng.standard_normal((S, D)) * 10.0 ** rng.uniform(-3, 3, (S, 1))).astype(np.float16)
+    q = np.where(rng.random((S, G, 1)) < 0.5, 1, -1).astype(np.float16) * k
+    cache, slots = binding.alloc_cache(S, 32, 1, D), np.arange(S, dtype=np.int64) * 32
+    binding.itq3s_cache_append(None, dev(torch, k[:, 0]), dev(torch, v), None, None, cache, dev(torch, slots))
+    v = binding.itq3s_cache_read(cache, dev(torch, slots), dtype=torch.float32)[1].double().cpu().numpy()
+    all_q = np.ones((S, rows_of_one, G * D), dtype=np.float16)
+    all_q[:, -1] = q.reshape(S, -1)
+    starts = np.arange(S + 1, dtype=np.int32) * rows_of_one
+    got = binding.itq3s_cache_attention(dev(torch, all_q.reshape(-1, G * D)), cache, dev(torch, starts), dev(torch, np.ones(S, dtype=np.int32)), dev(torch, np.arange(S, dtype=np.int32)[:, None]), max_q=rows_of_one, max_kv=32)
+    got = got.double().cpu().numpy().reshape(S, rows_of_one, G, D)
+    assert not got[:, :-1].any()
+    for s in range(S):
+        most = plain.bound(v[s], float(np.linalg.norm(v[s])), 0.0)
+        assert np.all(np.linalg.norm(got[s, -1] - v[s], axis=1) <= most)
