@@ -139,11 +139,11 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
         floatx16 o[D / 32];
         const bool there = row < total;
         const int i = there ? row / a.group : 0, hq = head * a.group + (there ? row % a.group : 0), see = !there ? 0 : a.causal ? i + 1 : len;
-        // A row's reference m is a score's product with the scale, rounded; a weight's exponent is exact, so it holds what the rounding
-        // left, and of a score of 2^28 that alone is more than fp16 has.  Once a row of the wavefront is beyond kFar, references
-        // are far + rest, which is exact, every tile goes through the branch that moves them, and what the weights are made of is there
-        // made relative to them: m is 0 then, unit 1.  (So nothing is done for it elsewhere.)
-        float m = kNoRow, far = 0.f, rest = 0.f, l = 0.f, unit = a.scale, room = kHeadroom;
+        // A row's reference is m + far * scale; one of them is 0.  m is a score's product with the scale, rounded, and a weight's exponent the
+        // exact difference from it: that holds what the rounding left, of a score of 2^28 more than fp16 has.  So where a row passes
+        // kFar its reference is its largest score before the scale, taken off the others before they are scaled.  room is how far
+        // scores may be above m: kHeadroom, or minus infinity (every tile moves references) once a row of the wavefront is there.
+        float m = kNoRow, far = 0.f, l = 0.f, room = kHeadroom;
         {
             const half8* const p = reinterpret_cast<const half8*>(a.Q + (int64_t)(first + i) * a.ldq + (int64_t)hq * D + 8 * hi);
 #pragma unroll
@@ -175,25 +175,16 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
             for (int x = 1; x < 16; ++x) top = __builtin_fmaxf(top, s[x]);
             if (__builtin_amdgcn_ballot_w64(top * a.scale > m + room) != 0) {
                 top = __builtin_fmaxf(top, xor_lane_f32(top, 32));
-                const bool was_far = room < 0.f;
-                const float t = top * a.scale, old = was_far ? far : m;
-                float n = __builtin_fmaxf(old, t), left = 0.f;
-                const bool is_far = was_far || __builtin_amdgcn_ballot_w64(__builtin_fabsf(n) > kFar && n > 0.1f * kNoRow) != 0;
-                if (is_far) {
+                float n = __builtin_fmaxf(__builtin_fmaf(far, a.scale, m), top * a.scale), far_n = 0.f;
+                if (room < 0.f || __builtin_amdgcn_ballot_w64(__builtin_fabsf(n) > kFar && n > 0.1f * kNoRow) != 0) {
                     asm volatile("");
-                    if (__builtin_fabsf(n) > kFar) {
-                        const float t_left = __builtin_fmaf(top, a.scale, -t);
-                        const bool higher = t > old || (t == old && t_left > rest);
-                        n = higher ? t : old, left = higher ? t_left : rest;
-                    }
+                    room = -__builtin_inff();
+                    if (__builtin_fabsf(n) > kFar && n > 0.1f * kNoRow) n = 0.f, far_n = far != 0.f ? __builtin_fmaxf(far, top) : top;
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, -n) - left;
-                    far = n, m = 0.f, unit = 1.f, room = -__builtin_inff();
-                } else {
-                    m = n;
+                    for (int x = 0; x < 16; ++x) s[x] -= far_n;
                 }
-                const float f = __builtin_amdgcn_exp2f((old - n) + (rest - left));
-                rest = left;
+                const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(far - far_n, a.scale, m - n));
+                m = n, far = far_n;
                 l *= f;
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) o[x] *= f;
@@ -201,7 +192,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
             half8 p[2];  // weights: fp16, at most 2^8, one rounding each; their sum in fp32
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], unit, -m));
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], a.scale, -m));
                 l += e;
                 p[x / 8][x % 8] = (_Float16)e;
             }
@@ -211,7 +202,6 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
                 for (int x = 0; x < D / 32; ++x) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_part<D>(lds, va, k, x), p[k], o[x], 0, 0, 0);
         }
         l += xor_lane_f32(l, 32);
-        if (room < 0.f) m = far;
         if constexpr (kParts == 2) {
             sync_copies();
             floatx4* const meet = reinterpret_cast<floatx4*>(lds) + group * ((D / 8 + 1) * 64) + lane;
@@ -220,13 +210,12 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
                 for (int x = 0; x < D / 32; ++x)
 #pragma unroll
                     for (int y = 0; y < 4; ++y) meet[(4 * x + y) * 64] = floatx4{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
-                meet[D / 8 * 64] = floatx4{m, l, rest, 0.f};
+                meet[D / 8 * 64] = floatx4{m, l, far, 0.f};
             }
             sync_copies();
             if (part == 1) continue;
             const floatx4 ml = meet[D / 8 * 64];
-            const float n = __builtin_fmaxf(m, ml[0]), d0 = (m - n) + rest, d1 = (ml[0] - n) + ml[2], d = __builtin_fmaxf(d0, d1);
-            const float f0 = __builtin_amdgcn_exp2f(d0 - d), f1 = __builtin_amdgcn_exp2f(d1 - d);
+            const float d = __builtin_fmaf(far - ml[2], a.scale, m - ml[0]), f0 = __builtin_amdgcn_exp2f(d < 0.f ? d : 0.f), f1 = __builtin_amdgcn_exp2f(d > 0.f ? -d : 0.f);
             l = l * f0 + ml[1] * f1;
 #pragma unroll
             for (int x = 0; x < D / 32; ++x)
