@@ -52,6 +52,31 @@ def test_rows_far_beyond_the_largest_step_keep_their_signs(gpu, D, normed):
     assert int(flags.item()) == binding.FLAG_SCALE_SAT
 
 
+@pytest.mark.parametrize("kind", ["turned", "normed"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_keys_in_fp16_are_rounded_once(gpu, D, kind):
+    """Products of fp32 keys and an fp32 factor are exact in 64 bits, and one in 2^14 lies so near a border of fp16 that a rounding to
+    fp32 on the way would move it there.  Every value is the 64-bit one's nearest."""
+    torch, binding = gpu
+    rng = np.random.default_rng(D)
+    T, H = 4096, 512 // D
+    k = rng.standard_normal((T, H * D)).astype(np.float32)
+    if kind == "turned":  # by no angle, with a gain
+        gain = np.float32(1.2345678)
+        _, got = binding.itq3s_cache_append(None, dev(torch, k), None, torch.zeros(T, dtype=torch.int32, device="cuda"), binding.itq3s_rope_frequencies(D).cuda(), head_dim=D, gain=float(gain))
+        want = k.astype(np.float64) * np.float64(gain)
+    else:  # rows of +-1, whose norm is 1 with no eps
+        k = np.where(k > 0, 1, -1).astype(np.float16)
+        weight = (rng.standard_normal(D) * 2.0 ** rng.integers(-20, 15, D)).astype(np.float32)
+        tie = (1 + (2 * rng.integers(0, 1024, D) + 1) * 2.0**-11) * 2.0 ** rng.integers(-10, 10, D)
+        weight[::2] = tie[::2]  # to even
+        weight[:8] = 65520, 65519.996, 1e30, np.inf, 2.0**-25, 2.0**-25 * (1 + 2.0**-23), 1e-30, 0.0  # its ends
+        _, got = binding.itq3s_cache_append(None, dev(torch, k), None, head_dim=D, k_norm=dev(torch, weight), eps=0.0)
+        want = (k.reshape(T, H, D) * weight.astype(np.float64)).reshape(T, H * D)
+    with np.errstate(over="ignore"):
+        assert np.array_equal(got.cpu().numpy(), want.astype(np.float16))
+
+
 # ---- scores of every size
 
 
