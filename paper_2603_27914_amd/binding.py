@@ -510,14 +510,17 @@ def alloc_cache(pages, page_tokens, kv_heads, head_dim, device="cuda"):
 _U8, _I32, _I64, _F16T, _F32T, _F64T = torch.uint8, torch.int32, torch.int64, torch.float16, torch.float32, torch.float64
 
 
+_PAGE_TOKENS, _HEAD_DIMS = frozenset(2**i for i in range(5, 17)), frozenset((64, 128, 256))
+
+
 def _need_cache(cache):
-    """-> the descriptor of a cache, checked against its tensor (the library checks the layout)."""
+    """-> the descriptor of a cache, checked against its tensor."""
     data, page_tokens, kv_heads, head_dim = cache
     if data.dtype != _U8 or not data.is_contiguous():
         raise Itq3sError("the cache's data must be a contiguous uint8 tensor")
+    if page_tokens not in _PAGE_TOKENS or head_dim not in _HEAD_DIMS or not 0 < kv_heads <= 1024:
+        raise Itq3sError("bad cache: page_tokens a power of two from 32 to 65536, head_dim 64, 128 or 256, kv_heads 1 to 1024")
     one = kv_heads * (page_tokens // 32) * (32 * head_dim + 128)
-    if one <= 0 or page_tokens % 32:
-        raise Itq3sError("bad cache: page_tokens a power of two from 32 to 65536, head_dim 64, 128 or 256, kv_heads positive")
     pages, rest = divmod(data.numel(), one)
     if pages == 0 or rest:
         raise Itq3sError("the cache holds %d bytes: not whole pages of %d" % (data.numel(), one))
