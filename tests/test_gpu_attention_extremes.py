@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from tests import attention_plain as plain
+from tests import test_gpu_attention as base
 
 pytestmark = pytest.mark.gpu
 
@@ -242,3 +243,55 @@ def test_cached_sequences_of_one_token_give_its_value(gpu, rows_of_one, D, facto
     for s in range(S):
         most = plain.bound(v[s], float(np.linalg.norm(v[s])), 0.0)
         assert np.all(np.linalg.norm(got[s, -1] - v[s], axis=1) <= most)
+
+
+# ---- row starts that fall or leave the rows
+
+
+STARTS = [
+    # starts of a tensor of 8 rows, the rows of every sequence that they are cut to
+    ([4, 2, -7, 3, 900], [(4, 4), (2, 2), (0, 3), (3, 8)]),
+    ([900, 4, 5, -2], [(8, 8), (4, 5), (5, 5)]),
+    ([-2147483648, 2147483647], [(0, 8)]),
+    ([5, 5, 8, 2147483647], [(5, 5), (5, 8), (8, 8)]),
+]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("max_q", [1, 8])
+@pytest.mark.parametrize("starts,cut", STARTS)
+def test_cache_attention_cuts_starts_to_the_rows(gpu, starts, cut, max_q, D):
+    torch, binding = gpu
+    rng = np.random.default_rng(D)
+    T, H, G = 8, 2, 16
+    lens = [40 + 7 * s for s in range(len(cut))]
+    c, table, slots = base.fill(rng, lens, 32, H, D)
+    q = base.rows(rng, T, H * G, D, "f16")
+    out = torch.full((T, H * G * D), 2.0, dtype=torch.float16, device="cuda")
+    binding.itq3s_cache_attention(dev(torch, q), binding.Cache(dev(torch, c.data), 32, H, D), dev(torch, np.array(starts, dtype=np.int32)), dev(torch, np.array(lens, dtype=np.int32)), dev(torch, table), out=out, max_q=max_q)
+    got = out.double().cpu().numpy().reshape(T, H * G, D)
+    for s, (a, b) in enumerate(cut):
+        base.check_cache_attention(c, [slots[s]], q.reshape(T, H * G, D)[a:b], [0, b - a], [lens[s]], D**-0.5, got[a:b], G)
+    nobody = [i for i in range(T) if not any(a <= i < b for a, b in cut)]
+    assert np.all(got[nobody] == 2.0)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("starts,cut", STARTS)
+def test_prompt_attention_cuts_starts_to_the_rows(gpu, starts, cut, causal, D):
+    torch, binding = gpu
+    rng = np.random.default_rng(D)
+    T, H, G = 8, 2, 16
+    q, k, v = base.rows(rng, T, H * G, D, "f16", outliers=False), base.rows(rng, T, H, D, "f16"), base.rows(rng, T, H, D, "f16")
+    out = torch.full((T, H * G * D), 2.0, dtype=torch.float16, device="cuda")
+    binding.itq3s_prompt_attention(dev(torch, q), dev(torch, k), dev(torch, v), D, dev(torch, np.array(starts, dtype=np.int32)), causal=causal, out=out)
+    got, q, k, v = (x.astype(np.float64).reshape(T, -1, D) for x in (out.cpu().numpy(), q, k, v))
+    for a, b in cut:
+        for i in range(a, b):
+            for h in range(H * G):
+                end = i + 1 if causal else b
+                o, weight, reach = plain.attend(q[i, h], k[a:end, h // G], v[a:end, h // G], D**-0.5)
+                assert np.linalg.norm(got[i, h] - o) <= plain.bound(o, weight, reach)
+    nobody = [i for i in range(T) if not any(a <= i < b for a, b in cut)]
+    assert np.all(got[nobody] == 2.0)
