@@ -243,6 +243,9 @@ int itq3s_matmul_sub(const uint32_t *codes, const uint32_t *scales, const uint32
  * the input alone.  0.516 bytes a value at head_dim 128.  A row with a NaN or infinity is stored as zeros
  * (ITQ3S_FLAG_NONFINITE), a step beyond fp16 as 65504 (ITQ3S_FLAG_SCALE_SAT); rows whose largest |w| is below 2.2e-7 are zeros,
  * and steps below 6e-5 have fewer bits.
+ * What four bits lose: 10 to 12 % of a row's norm (N(0, 1) channels, also with two of them six times as large, which cost 20 % without
+ * the transform).  Attention of random queries over 1000 such tokens is off by 1 to 2 % of a value's norm: 15 to 20 % of the result's, since
+ * random values cancel.  Every operator here is exact up to its own roundings on what the cache holds.
  *   Blocks of 32 tokens of one kv head, 32 * head_dim + 128 bytes (D = head_dim; t = 0..31 the token of the block):
  *     keys   at 0     : digit of channel 8 w + j of token t in word t * D / 8 + w, nibble (j >> 1) + 4 (j & 1)
  *     values at 16 D  : token t = 16 a + 4 g + b, channel 64 h + 32 p + 16 n + c: nibble n of byte
@@ -308,8 +311,10 @@ int itq3s_cache_read(const itq3s_cache *cache, const int64_t *slots, int64_t T, 
  *            than ld_pages * page_tokens: that much, ITQ3S_FLAG_BAD_SLOT);  pages device, int32: a page that is not of
  *            the cache is taken for tokens that nobody sees, ITQ3S_FLAG_BAD_SLOT; entries behind a sequence's last token may be anything
  *   max_q, max_kv  the most rows and tokens of a sequence that the work is cut up for.  Longer sequences are computed all the same,
- *            slower; with max_q above T, T is meant
- *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs * kv_heads up to 2^22;  |scale| up to 2^40;  out overlaps no input
+ *            slower, and so are shorter ones (64 of 1500 to 2500 tokens, one row each, 64 query heads: 29 us, with max_q 64 92); with
+ *            max_q above T, T is meant
+ *   ld_pages * page_tokens and T * (q_heads / kv_heads) up to 2^30, seqs * kv_heads up to 2^22;  |scale| up to 2^40 (scores of
+ *   any size that this allows are within fp32, and largest ones have weight 1);  out overlaps no input
  *   workspace device, 256-byte aligned, itq3s_cache_attention_workspace_bytes() of the same sizes on the same device (never 0); as for itq3s_matmul */
 size_t itq3s_cache_attention_workspace_bytes(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv);
 int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, const itq3s_cache *cache, const int32_t *q_starts,

@@ -679,7 +679,8 @@ def itq3s_cache_attention(q, cache, q_starts, kv_lens, pages, scale=None, max_q=
     pages[s] (all int32, [seqs + 1], [seqs], [seqs, pages]).  -> out, as q.
 
     scale: 1 / sqrt(head_dim) if not given; max_q, max_kv: the most rows and tokens of a sequence to cut the work up for (T and what the
-    page table has room for if not given); workspace: uint8, allocated here if not given."""
+    page table has room for if not given: any is right, near ones are fast, and for a batch of single rows T is far from 1);
+    workspace: uint8, allocated here if not given."""
     _need_here(q, cache[0], q_starts, kv_lens, pages, out, workspace, status_flags)
     desc = _need_cache(cache)
     if q.dim() != 2:

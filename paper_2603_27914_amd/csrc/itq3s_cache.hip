@@ -16,7 +16,7 @@
 // heads with the sines that it has worked out once.
 //
 // Measured: 11385 tokens, 64 normed query heads and 8 kv heads of 128, half of each rotated, fp16 (440 MB) 99 us, 4.4 TB/s; the
-// arithmetic in 64 bits takes the vector ALU for 71 % of that time, so neither the memory (a copy: 5.2 TB/s) nor the ALU
+// arithmetic in 64 bits takes the vector ALU for 72 % of that time, so neither the memory (a copy: 5.2 TB/s) nor the ALU
 // is far away.  One token 4.4 us, most of it a launch and two loads that wait for each other (position, then row).
 #include <type_traits>
 

@@ -22,8 +22,8 @@
 // 31 us, 4.5 TB/s (a copy: 5.2); one of 131072 tokens, 8 kv heads, in 25 us and 5 for the join.  A wavefront waits for memory
 // for a third of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four a SIMD), or
 // two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
-// 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (63 and 33 %
-// of it): 512 rows of 64 heads over 16500 tokens 351 us, 776 TFLOP/s.  Unpacking once for four wavefronts into LDS saves a
+// 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (66 and 33 %
+// of it): 512 rows of 64 heads over 16500 tokens 350 us with its join, 778 TFLOP/s (once the clock has settled; the first calls take 40 more).  Unpacking once for four wavefronts into LDS saves a
 // third of the vector instructions and took 345 to 385 us, other sizes 5 % more than
 // this: it leaves room for few more wavefronts, and they wait for each other.  (The older of two workgroups on a unit takes 270 us, the younger
 // 355; one of eight wavefronts that keep step takes as long.)
@@ -769,7 +769,8 @@ Plan plan_of(int64_t T, int64_t seqs, int q_heads, int kv_heads, int head_dim, i
     // sequence, 8 kv heads, of 120 tokens 8.7 and 8.2, 250 9.3 and 10.8, 1000 11.6 and 12.2, 2000 14.5 and 12.5; 8 of 2000
     // 14.7 and 15.8, of 4000 20.5 and 18.1; 32 of 6000 47 and 52; 48 of 250 16.3 and 16.2, of 120 15.1 and 9.9.
     p.wide = p.share == Share::blocks && rows <= 16 && head_dim <= 128 && blocks > 4 && units <= cus && blocks <= 32 + units * 256 / cus;
-    // Else as many parts as give every unit two workgroups (three of Share::tiles, for their ragged batches: above 81, with two 89).
+    // Else as many parts as give every unit two workgroups (three of Share::tiles, for their ragged batches: 81 us above, with two 89.  LDS
+    // has room for two at a time with 128 channels, for one with 256: the third begins where one of short sequences has ended).
     // Four a unit, which also fit where a workgroup has four wavefronts, measured for 8 kv heads of 128: one sequence of
     // 131072 tokens 41.9 us, with two 40.7; 64 of 1000 23.9 and 18.9; one of 16000 20.7 and 16.2; 16 of 2500 with 32 heads
     // 40.2 and 36.7.  One a unit: 131072 tokens 45.8 us.  (Sequences have rows for so many tiles at most.)
