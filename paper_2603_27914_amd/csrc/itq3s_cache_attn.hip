@@ -188,10 +188,19 @@ struct Mantissas {
 __device__ __forceinline__ half8 key_operand(uint32_t w, const Mantissas& m) {
     return as_halves((w & 0x000f000fu) | m.low, (w & 0x00f000f0u) | m.high, ((w >> 8) & 0x000f000fu) | m.low, ((w >> 8) & 0x00f000f0u) | m.high);
 }
-// Stored digits of values, as subnormal fp16: n 2^-24, or n 2^-20 for the upper nibbles, exactly what the matrix cores take them for
-// (and 8 less, where few rows share blocks).
+// Stored digits of values, as subnormal fp16: n 2^-24, or n 2^-20 for the upper nibbles, exactly what the matrix cores take them for.
+// Where few rows share blocks, as digits c themselves: in the mantissa of 1024 or of 64, and 1032 or 72 off that.
 __device__ __forceinline__ half8 value_operand_low(uint32_t u, uint32_t w) { return as_halves(u & 0x000f000fu, (u >> 8) & 0x000f000fu, w & 0x000f000fu, (w >> 8) & 0x000f000fu); }
 __device__ __forceinline__ half8 value_operand_high(uint32_t u, uint32_t w) { return as_halves(u & 0x00f000f0u, (u >> 8) & 0x00f000f0u, w & 0x00f000f0u, (w >> 8) & 0x00f000f0u); }
+
+__device__ __forceinline__ half8 centred_operand_low(uint32_t u, uint32_t w, const Mantissas& m) {
+    const half8 offset = as_halves(0xe408e408u, 0xe408e408u, 0xe408e408u, 0xe408e408u);  // -1032
+    return as_halves((u & 0x000f000fu) | m.low, ((u >> 8) & 0x000f000fu) | m.low, (w & 0x000f000fu) | m.low, ((w >> 8) & 0x000f000fu) | m.low) + offset;
+}
+__device__ __forceinline__ half8 centred_operand_high(uint32_t u, uint32_t w, const Mantissas& m) {
+    const half8 offset = as_halves(0xd480d480u, 0xd480d480u, 0xd480d480u, 0xd480d480u);  // -72
+    return as_halves((u & 0x00f000f0u) | m.high, ((u >> 8) & 0x00f000f0u) | m.high, (w & 0x00f000f0u) | m.high, ((w >> 8) & 0x00f000f0u) | m.high) + offset;
+}
 
 // The rotated queries of a wavefront's rows, as the products want them: lane (column l % 16, g = l / 16) holds channels
 // (D/4) g .. (D/4) (g + 1) - 1, scaled by a power of two into fp16's best range, in kParts parts of fp16 (two leave no
@@ -247,11 +256,12 @@ __device__ __forceinline__ void load_queries(const unsigned char* lds, uint32_t 
 }
 
 // O^T in the units of value_operand: accumulators of even channel tiles times 2^24, of odd ones 2^20.  With digits n = c + 8 each has
-// `eight` too much (of sum 8 P', in the even ones' units); the matrix cores cut the sum of a product's terms, which over a long context adds
-// up against that sum: a row of 131072 tokens comes out 6e-4 off.  So few rows, whose time is the memory's, take 8 off the digits
-// (kCentred: 3.3e-4, and 1 to 2 % of time), and many rows, whose time is the vector ALU's, do not (16500 tokens 4.5e-4, where
-// it were 4.1e-4 and 4 to 12 % of time; 2.1e-4 of each is the result's rounding to fp16).  Nor do sixteen wavefronts of a
-// short sequence (2.9e-4 either way).
+// `eight` too much (of sum 8 P', in the even ones' units).  The matrix cores cut the sum of a product's terms, subnormal ones at the place of
+// fp16's least normal number: a row of 131072 tokens comes out 6e-4 off.  So few rows, whose time is the memory's, have the digits c as
+// ordinary fp16 (kCentred: 2.9e-4, nothing is cut; with 8 taken off subnormal ones 3.3e-4 in the same time), and many rows, whose
+// time is the vector ALU's, do not (16500 tokens 4.5e-4, where it were 4.1e-4 and 4 to 12 % of time; queries in two parts
+// 3.6e-4 and 399 us instead of 347; 2.1e-4 of each is the result's rounding to fp16).  Nor do sixteen wavefronts of a short
+// sequence (3.0e-4 either way).
 template <int D, int CT>
 struct State {
     floatx4 o[D / 16][CT], eight[CT];
@@ -372,8 +382,8 @@ __device__ __forceinline__ void weights(const floatx4 (&s)[2][CT], u32x4 (&step)
 }
 
 template <int D, int CT, bool kCentred>
-__device__ __forceinline__ void products(const u32x4 (&v)[D / 64], const half8 (&p)[CT], State<D, CT>& st) {
-    const half8 eight = as_halves(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u), upper_eight = as_halves(0x00800080u, 0x00800080u, 0x00800080u, 0x00800080u);
+__device__ __forceinline__ void products(const u32x4 (&v)[D / 64], const half8 (&p)[CT], const Mantissas& mant, State<D, CT>& st) {
+    const half8 eight = as_halves(0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u);
     if constexpr (!kCentred)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) st.eight[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p[ct], st.eight[ct], 0, 0, 0);
@@ -381,8 +391,9 @@ __device__ __forceinline__ void products(const u32x4 (&v)[D / 64], const half8 (
     for (int h = 0; h < D / 64; ++h)
 #pragma unroll
         for (int pp = 0; pp < 2; ++pp) {
-            half8 lo = value_operand_low(v[h][2 * pp], v[h][2 * pp + 1]), hi = value_operand_high(v[h][2 * pp], v[h][2 * pp + 1]);
-            if constexpr (kCentred) lo -= eight, hi -= upper_eight;
+            half8 lo, hi;
+            if constexpr (kCentred) lo = centred_operand_low(v[h][2 * pp], v[h][2 * pp + 1], mant), hi = centred_operand_high(v[h][2 * pp], v[h][2 * pp + 1], mant);
+            else lo = value_operand_low(v[h][2 * pp], v[h][2 * pp + 1]), hi = value_operand_high(v[h][2 * pp], v[h][2 * pp + 1]);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 st.o[4 * h + 2 * pp][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, p[ct], st.o[4 * h + 2 * pp][ct], 0, 0, 0);
@@ -556,7 +567,7 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
                 __builtin_amdgcn_s_setprio(0);
                 load_steps<D>(next.at, r.s, lane);
                 __builtin_amdgcn_sched_barrier(0);
-                products<D, CT, kCentred>(r.v, p, st);
+                products<D, CT, kCentred>(r.v, p, mant, st);
                 __builtin_amdgcn_sched_barrier(0);
                 load_values<D>(next.at, r.v, lane);
                 __builtin_amdgcn_sched_barrier(0);
@@ -573,8 +584,10 @@ __global__ void __launch_bounds__(64 * kWaves, CT == 1 && D <= 128 ? 4 : 2) cach
             st.m[ct] = __builtin_fmaf(st.far[ct], q.unit[ct], st.m[ct]);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                if constexpr (!kCentred) st.o[c][ct] -= c % 2 == 0 ? st.eight[ct] : st.eight[ct] * 16.f;
-                st.o[c][ct] *= c % 2 == 0 ? 16777216.f : 1048576.f;
+                if constexpr (!kCentred) {
+                    st.o[c][ct] -= c % 2 == 0 ? st.eight[ct] : st.eight[ct] * 16.f;
+                    st.o[c][ct] *= c % 2 == 0 ? 16777216.f : 1048576.f;
+                }
             }
         }
         if constexpr (!kOwn) {

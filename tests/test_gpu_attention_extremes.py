@@ -295,3 +295,35 @@ def test_prompt_attention_cuts_starts_to_the_rows(gpu, starts, cut, causal, D):
                 assert np.linalg.norm(got[i, h] - o) <= plain.bound(o, weight, reach)
     nobody = [i for i in range(T) if not any(a <= i < b for a, b in cut)]
     assert np.all(got[nobody] == 2.0)
+
+
+# ---- sums of digits
+
+
+@pytest.mark.parametrize("G", [8, 32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_sums_of_values_that_cancel_are_exact(gpu, D, G):
+    """Weights that are powers of two, 1 to 2^4 and, of two tokens of each block whose values are opposite, 2^15 (but for some 2^-21 of them, which
+    fp16 rounds away): sums of weights times digits have 24 bits at most, so fp32 holds them however much they cancel (few rows, where
+    the blocks are shared).  The transform's eight sums at most, the sum of weights and the last factor round to fp32, some twelve
+    times what is added; the result rounds once."""
+    torch, binding = gpu
+    rng = np.random.default_rng(D)
+    n = 2016
+    c = plain.PlainCache(63, 32, 1, D)
+    digits, power = rng.integers(-7, 8, (n, D)), rng.integers(-8, -3, n)
+    for b in range(0, n, 32):
+        i, j = b + rng.choice(32, 2, replace=False)
+        power[[i, j]], digits[j] = 7, -digits[i]
+    for t in range(n):
+        c.put(t, 0, False, np.full(D, power[t]), np.float16(0.125))  # in channel 0: 0.125 sqrt(D) times the power
+        c.put(t, 0, True, digits[t], np.float16(4096.0))
+    q = np.zeros((1, G, D), dtype=np.float16)
+    q[..., 0] = 1.0
+    out = binding.itq3s_cache_attention(dev(torch, q.reshape(1, -1)), binding.Cache(dev(torch, c.data), 32, 1, D), dev(torch, np.array([0, 1], dtype=np.int32)), dev(torch, np.array([n], dtype=np.int32)),
+                                        dev(torch, np.arange(63, dtype=np.int32)[None]), max_q=1, max_kv=n, scale=float(np.log(2) / (0.125 * np.sqrt(D))))
+    weight = 2.0**power
+    total = weight @ digits
+    want, unit = plain.turned(total) * 4096 / weight.sum(), 4096 / weight.sum() / np.sqrt(D)
+    got = out.double().cpu().numpy().reshape(G, D)
+    assert np.all(np.abs(got - want) <= 1.01 * 2.0**-11 * np.abs(want) + 12 * 2.0**-24 * unit * np.abs(total).sum() + 2.0**-25), np.abs(got - want).max() / np.abs(want).max()
