@@ -24,9 +24,15 @@ PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
 # where the way to the first load is not what counts it only costs: quantizer 0.12 us of every call (4.7 -> 4.8)
 NO_PRELOAD = ("itq3s_quantize.hip",)
 
+# matrix products among the ordinary registers: where a kernel has room for more than 256, they would go through accumulation
+# registers, with a copy for each (prompts of 2000 tokens, 16 and 8 heads of 256: 128 copies a tile, 65 us)
+PRODUCTS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+WITH_PRODUCTS = ("itq3s_prompt.hip",)
+
 
 def flags(source):
-    return FLAGS + ([] if os.path.basename(source) in NO_PRELOAD else PRELOAD)
+    name = os.path.basename(source)
+    return FLAGS + ([] if name in NO_PRELOAD else PRELOAD) + (PRODUCTS if name in WITH_PRODUCTS else [])
 
 
 def build_lib(force=True, verbose=False):

@@ -15,6 +15,8 @@
 // us where this took 546, 8192 tokens, 32 query and 8 kv heads of 128.)  That takes 535 us by now, 1.03 PFLOP/s, where a matrix product
 // of 8192 x 8192 x 8192 reaches 1.21; the matrix pipes are busy for 60 % of the time, the vector ALU for 47 %, and the clock is down
 // to 1.66 GHz by what that draws.  Neither products nor softmax first (wavefront priorities) helped: 556 and 562 us where it was 554.
+#include <type_traits>
+
 #include "itq3s_attention.h"
 #include "itq3s_cache.h"
 
@@ -73,6 +75,27 @@ __device__ __forceinline__ half8 value_part(const unsigned char* lds, uint32_t a
     return half8{u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
 }
 
+// A tile of values with zeros for those that are not finite, 16 bytes of 1024 a lane, and the first token that has one (none: one beyond all).
+template <int D>
+__device__ __forceinline__ int copy_finite_values(const unsigned char* tile, unsigned char* to) {
+    int first = 1 << 30;
+#pragma unroll 1
+    for (int u = kTile * D * 2 / 1024 - 1; u >= 0; --u) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(tile + 1024 * u);
+        bool finite = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool lo = (v[i] & 0x7c00u) != 0x7c00u, hi = (v[i] & 0x7c000000u) != 0x7c000000u;
+            v[i] &= (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
+            finite = finite && lo && hi;
+        }
+        *reinterpret_cast<u32x4*>(to + 1024 * u) = v;
+        const uint64_t bad = __builtin_amdgcn_ballot_w64(!finite);
+        if (bad != 0) first = (u * 1024 + (int)__builtin_ctzll(bad) * 16) / (D * 2);
+    }
+    return first;
+}
+
 // Copies global -> LDS, 16 bytes a lane: lane l to lds + 16 l from its offset; zeros from beyond the descriptor's range.  (m0 is
 // reserved and cannot be named as clobbered: nothing else in a kernel with these copies uses it, which a test reads from
 // the assembly.  What the copies write, sync() orders for the compiler as well.)
@@ -86,7 +109,7 @@ __device__ __forceinline__ u32x4 rows_descriptor(const _Float16* p, int64_t byte
 }
 
 // Wavefronts a SIMD: what LDS has room for, three for 128 channels.
-constexpr int waves_of_simd(int D, int waves, int parts) { return D == 64 ? 4 : parts == 2 ? (D == 128 ? 2 : 1) : D == 128 ? 3 : waves / 2; }
+constexpr int waves_of_simd(int D, int waves, int parts) { return D == 64 ? 4 : parts == 2 ? (D == 128 ? 2 : 1) : D == 128 ? waves / 2 + waves / 4 : waves / 2; }
 
 // kParts = 2: the wavefronts of one half take the tiles 0, 2, 4, ..., the others, with the same rows, 1, 3, 5, ..., and join in the end.
 template <int D, int kWaves, int kParts>
@@ -94,10 +117,10 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     constexpr int kThreads = 64 * kWaves, kTokens = kTile * kParts, kChunks = kTokens * D / 8 / kThreads, kTileBytes = kTile * D * 2, kStepBytes = kParts * kTileBytes, kValues = 2 * kStepBytes;
     constexpr int kStep = kThreads * 8 / D;  // rows between a thread's chunks
     __shared__ __align__(1024) unsigned char lds[4 * kStepBytes];  // keys of two steps, values of two
+    __shared__ int not_finite;                                     // some result of the workgroup's is not
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = lane_id(), hi = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int part = kParts == 1 ? 0 : wave / (kWaves / kParts), group = kParts == 1 ? wave : wave % (kWaves / kParts);  // which tiles and which rows
-    const uint32_t k_place = key_place<D>(lane) + part * kTileBytes, v_place = value_place<D>(lane) + kValues + part * kTileBytes;
     int id = blockIdx.x;
     const int head = id % a.kv_heads;
     id /= a.kv_heads;
@@ -110,8 +133,13 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     const int count = (total + kRows - 1) / kRows;
     const _Float16* const kb = a.K + (int64_t)first * a.ldk + (int64_t)head * D;
     const _Float16* const vb = a.V + (int64_t)first * a.ldv + (int64_t)head * D;
-    // the last rows have the most to see: they begin
-    for (int tile = count - 1 - id / a.seqs; tile >= 0; tile -= a.tiles) {
+    // The rows of a tile; with care for values that are not finite (see below).
+    auto rows_of = [&](int tile, auto with_care) {
+        constexpr bool careful = decltype(with_care)::value;
+        int lane = lane_id();
+        if constexpr (careful) asm volatile("" : "+v"(lane));  // (what hangs on it is not kept for this)
+        const int tid = wave * 64 + lane, hi = lane >> 5, col = lane & 31;
+        const uint32_t k_place = key_place<D>(lane) + part * kTileBytes, v_place = value_place<D>(lane) + kValues + part * kTileBytes;
         const int row0 = tile * kRows + group * 32, row = row0 + col;
         const int last_row = (tile + 1) * kRows < total ? (tile + 1) * kRows - 1 : total - 1;
         const int tokens = a.causal ? last_row / a.group + 1 : len;  // that the workgroup needs
@@ -156,15 +184,35 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
         int buffer = 0;
         for (int step = 0; step < tokens; step += kTokens, buffer ^= 1) {
             sync_copies();  // this step's tiles are there, and the others' place is free
-            load(step + kTokens, buffer ^ 1);
+            if constexpr (!careful) {
+                load(step + kTokens, buffer ^ 1);
+            } else {
+                load(step, buffer);
+                sync_copies();
+            }
             const int t0 = step + part * kTile;
             if (t0 >= mine) continue;
-            const uint32_t ka = k_place + buffer * kStepBytes, va = v_place + buffer * kStepBytes;
+            const uint32_t ka = k_place + buffer * kStepBytes;
+            uint32_t va = v_place + buffer * kStepBytes;
+            if (careful && t0 + kTile > all) {
+                // (all wavefronts that come here between two barriers write the same)
+                unsigned char* const values = lds + kValues + part * kTileBytes + lane * 16;
+                if (t0 + copy_finite_values<D>(values + buffer * kStepBytes, values + (buffer ^ 1) * kStepBytes) < see) l = __builtin_nanf("");
+                va = v_place + (buffer ^ 1) * kStepBytes;
+            }
             floatx16 s;
 #pragma unroll
             for (int x = 0; x < 16; ++x) s[x] = 0.f;
+            half8 next = key_part<D>(lds, ka, 0);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_part<D>(lds, ka, k), q[k], s, 0, 0, 0);
+            for (int k = 0; k < D / 16; ++k) {
+                const half8 now = next;
+                if (k + 1 < D / 16) next = key_part<D>(lds, ka, k + 1);
+                // (where no other wavefront's products are there in the meantime, keys are read a product ahead)
+                if constexpr (waves_of_simd(D, kWaves, kParts) == 1) __builtin_amdgcn_sched_barrier(0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, q[k], s, 0, 0, 0);
+                if constexpr (waves_of_simd(D, kWaves, kParts) == 1) __builtin_amdgcn_sched_barrier(0);
+            }
             if (t0 + kTile > all) {
                 asm volatile("");  // (a branch stays one: few tiles are cut)
 #pragma unroll
@@ -213,30 +261,48 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
                 meet[D / 8 * 64] = floatx4{m, l, far, 0.f};
             }
             sync_copies();
-            if (part == 1) continue;
-            const floatx4 ml = meet[D / 8 * 64];
-            const float d = __builtin_fmaf(far - ml[2], a.scale, m - ml[0]), f0 = __builtin_amdgcn_exp2f(d < 0.f ? d : 0.f), f1 = __builtin_amdgcn_exp2f(d > 0.f ? -d : 0.f);
-            l = l * f0 + ml[1] * f1;
+            if (part == 0) {
+                const floatx4 ml = meet[D / 8 * 64];
+                const float d = __builtin_fmaf(far - ml[2], a.scale, m - ml[0]), f0 = __builtin_amdgcn_exp2f(d < 0.f ? d : 0.f), f1 = __builtin_amdgcn_exp2f(d > 0.f ? -d : 0.f);
+                l = l * f0 + ml[1] * f1;
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x)
+                for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const floatx4 v = meet[(4 * x + y) * 64];
+                    for (int y = 0; y < 4; ++y) {
+                        const floatx4 v = meet[(4 * x + y) * 64];
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) o[x][4 * y + z] = o[x][4 * y + z] * f0 + v[z] * f1;
-                }
+                        for (int z = 0; z < 4; ++z) o[x][4 * y + z] = o[x][4 * y + z] * f0 + v[z] * f1;
+                    }
+            }
         }
         const float f = l == 0.f ? 0.f : 1.f / l;
-        if (there) {
+        half2v zeros = half2v{(_Float16)0.f, (_Float16)0.f};
+        asm volatile("" : "+s"(zeros));  // (for the compiler any number)
+        float none = 0.f;                // unless a result is not finite
+        if (there && part == 0) {
             _Float16* const out = a.out + (int64_t)(first + i) * a.ldo + (int64_t)hq * D + 4 * hi;
 #pragma unroll
             for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    *reinterpret_cast<half4*>(out + 32 * x + 8 * y) = half4{(_Float16)(o[x][4 * y] * f), (_Float16)(o[x][4 * y + 1] * f), (_Float16)(o[x][4 * y + 2] * f), (_Float16)(o[x][4 * y + 3] * f)};
+                for (int y = 0; y < 4; ++y) {
+                    const half4 h = half4{(_Float16)(o[x][4 * y] * f), (_Float16)(o[x][4 * y + 1] * f), (_Float16)(o[x][4 * y + 2] * f), (_Float16)(o[x][4 * y + 3] * f)};
+                    *reinterpret_cast<half4*>(out + 32 * x + 8 * y) = h;
+                    none = __builtin_amdgcn_fdot2(half2v{h[0], h[1]}, zeros, none, false);
+                    none = __builtin_amdgcn_fdot2(half2v{h[2], h[3]}, zeros, none, false);
+                }
         }
-    }
+        if (!careful && a.causal && __builtin_amdgcn_ballot_w64(!(none == 0.f)) != 0) not_finite = 1;
+    };
+    not_finite = 0;
+    // the last rows have the most to see: they begin
+    const int last = count - 1 - id / a.seqs;
+    for (int tile = last; tile >= 0; tile -= a.tiles) rows_of(tile, std::false_type());
     sync_copies();  // (the copies behind the last tile are into this workgroup's LDS)
+    // A weight of 0 keeps a value from rows that do not see it, unless it is not finite.  So where results are not, the workgroup takes its rows
+    // once more: in tiles that not all rows see, such values are zeros (a copy in the other step's place, so nothing is loaded ahead), and
+    // the rows that do see one are no numbers.  (To look at values beforehand costs every prompt 1 to 10 %, to look at results 0 to 1.)
+    if (__builtin_amdgcn_readfirstlane(not_finite) != 0)
+        for (int tile = last; tile >= 0; tile -= a.tiles) rows_of(tile, std::true_type());
 }
 
 template <int D, int kWaves, int kParts>

@@ -327,3 +327,42 @@ def test_sums_of_values_that_cancel_are_exact(gpu, D, G):
     want, unit = plain.turned(total) * 4096 / weight.sum(), 4096 / weight.sum() / np.sqrt(D)
     got = out.double().cpu().numpy().reshape(G, D)
     assert np.all(np.abs(got - want) <= 1.01 * 2.0**-11 * np.abs(want) + 12 * 2.0**-24 * unit * np.abs(total).sum() + 2.0**-25), np.abs(got - want).max() / np.abs(want).max()
+
+
+# ---- what is not finite, where a row does not see it
+
+
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_heads,kv_heads,lens", [(4, 2, [70, 33, 2]), (2, 2, [300]), (8, 1, [250, 40]), (64, 8, [530, 12, 300]), (7, 1, [100, 41]), (5, 1, [500, 260])])
+def test_what_is_not_finite_stays_behind_the_mask(gpu, q_heads, kv_heads, lens, D, what):
+    """A NaN or an infinity in a token of a prompt is NaN in the rows that see it and in no other, of that head's group alone."""
+    torch, binding = gpu
+    rng = np.random.default_rng(D + q_heads)
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T, G = int(starts[-1]), q_heads // kv_heads
+    x = {"q": base.rows(rng, T, q_heads, D, "f16", outliers=False), "k": base.rows(rng, T, kv_heads, D, "f16"), "v": base.rows(rng, T, kv_heads, D, "f16")}
+    clean = {n: x[n].astype(np.float64).reshape(T, -1, D) for n in "kv"}
+    first = np.full((len(lens), kv_heads), 10**9)
+    for s, n in enumerate(lens):
+        for h in range(kv_heads):
+            if n > 1 and (s + h) % 3 != 2:
+                bad = int(rng.integers(1, n))
+                first[s, h] = bad
+                for t in {bad, *(int(i) for i in rng.integers(bad, n, 3))}:
+                    x[what][starts[s] + t, h * D + rng.integers(0, D)] = rng.choice([np.nan, np.inf, -np.inf])
+                if what == "k":  # an infinite key is an infinite score, or one of minus infinity: not a number whatever the query
+                    x[what][starts[s] + bad, h * D : h * D + 2] = np.inf, -np.inf
+                    x["q"].reshape(T, -1, D)[starts[s] + bad :, h * G : (h + 1) * G, :2] = 1.0
+    clean["q"] = x["q"].astype(np.float64).reshape(T, -1, D)
+    got = binding.itq3s_prompt_attention(*(dev(torch, x[n]) for n in "qkv"), D, dev(torch, starts)).double().cpu().numpy().reshape(T, q_heads, D)
+    for s, (a, b) in enumerate(zip(starts[:-1], starts[1:])):
+        for h in rng.choice(q_heads, min(q_heads, 6), replace=False):
+            bad = first[s, h // G]
+            for i in range(b - a):
+                if i >= bad:
+                    # a value's infinity stays one where only that reached the row
+                    assert np.isnan(got[a + i, h]).all() if what == "k" else not np.isfinite(got[a + i, h]).all()
+                elif b - a < 100 or bad - i < 40 or i % 16 == 0:
+                    o, weight, reach = plain.attend(clean["q"][a + i, h], clean["k"][a : a + i + 1, h // G], clean["v"][a : a + i + 1, h // G], D**-0.5)
+                    assert np.linalg.norm(got[a + i, h] - o) <= plain.bound(o, weight, reach), (s, h, i, bad)
