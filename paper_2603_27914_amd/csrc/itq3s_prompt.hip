@@ -13,7 +13,7 @@
 // Many: three workgroups of four wavefronts a compute unit: nothing in a wavefront overlaps its products with its exponentials, the
 // others do.  (One wavefront a SIMD with 64 rows, which reads LDS half as often, and its two halves interleaved by hand: 606
 // us where this took 546, 8192 tokens, 32 query and 8 kv heads of 128.)  That takes 535 us by now, 1.03 PFLOP/s, where a matrix product
-// of 8192 x 8192 x 8192 reaches 1.21; the matrix pipes are busy for 60 % of the time, the vector ALU for 47 %, and the clock is down
+// of 8192 x 8192 x 8192 reaches 1.21; the matrix pipes are busy for 59 % of the time, the vector ALU for 47 %, and the clock is down
 // to 1.66 GHz by what that draws.  Neither products nor softmax first (wavefront priorities) helped: 556 and 562 us where it was 554.
 #include <type_traits>
 
