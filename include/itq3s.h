@@ -325,7 +325,7 @@ int itq3s_cache_attention(const void *Q, int64_t ldq, int64_t T, int q_heads, co
  * has rows starts[s] .. starts[s + 1] - 1 of Q, K, V and out; its row i sees its rows j <= i, or all of them if causal is 0.
  * Weights multiply in fp16, sums are fp32.  Rows of no sequence are neither read nor written.  In a sequence, a NaN or infinity
  * in K or V makes the rows that see it NaN (one in V: NaN or infinite, in its channel at least) and leaves the others as they are;
- * such a call takes up to three times as long.
+ * such a call takes twice as long.
  *   Q, out T x (q_heads * head_dim), K, V T x (kv_heads * head_dim), all fp16;  out must not overlap the inputs
  *   starts device, seqs + 1 int32, not falling (values beyond 0..T are cut to it)
  *   max_len  the most rows of a sequence that the work is cut up for (longer ones are computed all the same, slower)

@@ -23,8 +23,8 @@
 // for a third of its time there, and unpacking and softmax take the vector ALU for 40 %: more wavefronts (four a SIMD), or
 // two blocks on their way at once, gain nothing.  Short contexts: a chain of loads (lengths and page, block, ...): 1000 tokens
 // 10 us, where one token takes 7.  Many rows: the vector ALU and the matrix pipe, which share a SIMD's issue (66 and 33 %
-// of it): 512 rows of 64 heads over 16500 tokens 350 us with its join, 778 TFLOP/s (once the clock has settled; the first calls take 40 more).  Unpacking once for four wavefronts into LDS saves a
-// third of the vector instructions and took 345 to 385 us, other sizes 5 % more than
+// of it): 512 rows of 64 heads over 16500 tokens 350 us with its join, 778 TFLOP/s (once the clock has settled; the first calls take
+// 40 more).  Unpacking once for four wavefronts into LDS saves a third of the vector instructions and took 345 to 385 us, other sizes 5 % more than
 // this: it leaves room for few more wavefronts, and they wait for each other.  (The older of two workgroups on a unit takes 270 us, the younger
 // 355; one of eight wavefronts that keep step takes as long.)
 #include "itq3s_attention.h"
